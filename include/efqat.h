@@ -258,6 +258,64 @@ int efqat_network_qparam_adam(efqat_ctx* ctx, const efqat_adam* opt, int L, cons
 /* theta[i] = log2(s[i]) for i < n (Appendix A.2). */
 int efqat_log2_scale_init(efqat_ctx* ctx, const float* s, float* theta, int64_t n, efqat_stream_t stream);
 
+/* ---- activation checkpoints in 8 bits ------------------------------------------------- */
+/* What a training step has to remember of an activation between its forward and its backward
+ * pass, in 1 + 4/128 bytes per element instead of 2 or 4.  A checkpoint of x [M,C] holds
+ *   codes  int8 [M,C]  and  scales fp32 [M, ceil(C/128)]   (device, caller-owned, codes 16-byte aligned):
+ * every 128 consecutive elements of a row (the last group of a row may be shorter) share a scale.
+ * With a the largest |x| of a group:
+ *   scale = fl32(a / 127),  code = rne(fl32(x * fl32(127 / a))),  the element stands for fl32(code * scale).
+ * A group whose a is below 2^-100 (an all-zero group among them) is stored as zeros; a group that
+ * holds an infinity or a NaN has the scale NaN, so that all of it reads back as NaN: a non-finite
+ * activation is not lost on the way.  C % 16 == 0 and M >= 0 for every call that touches a
+ * checkpoint; tensors are dense, row-major, fp32 or bf16 (`dtype`), 16-byte aligned, and outputs
+ * do not overlap inputs.  Calls on zero rows succeed and touch nothing. */
+typedef struct {
+  int8_t* codes;
+  float* scales;
+} efqat_ckpt;
+/* Bytes of the two arrays of a checkpoint of [M,C]. */
+int efqat_ckpt_bytes(int64_t M, int64_t C, size_t* codes_bytes, size_t* scales_bytes);
+int efqat_ckpt_store(efqat_ctx* ctx, int dtype, const void* x, int64_t M, int64_t C, const efqat_ckpt* out,
+                     efqat_stream_t stream);
+int efqat_ckpt_load(efqat_ctx* ctx, int dtype, const efqat_ckpt* in, int64_t M, int64_t C, void* x,
+                    efqat_stream_t stream);
+
+/* GELU, y = x * Phi(x) with Phi the normal distribution function (the erf form).  fwd also writes
+ * the checkpoint of x when save_or_null is given; bwd computes dX = dY * (Phi(x) + x * phi(x)) from
+ * x itself or from its checkpoint (exactly one of x_or_null, saved_or_null); recompute forms y
+ * again from the checkpoint, e.g. as the X of the quantized layer behind it.  C % 8 == 0 where no
+ * checkpoint is involved. */
+int efqat_gelu_fwd(efqat_ctx* ctx, int dtype, const void* x, int64_t M, int64_t C, void* y,
+                   const efqat_ckpt* save_or_null, efqat_stream_t stream);
+int efqat_gelu_bwd(efqat_ctx* ctx, int dtype, const void* dY, const void* x_or_null,
+                   const efqat_ckpt* saved_or_null, int64_t M, int64_t C, void* dX, efqat_stream_t stream);
+int efqat_gelu_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* saved, int64_t M, int64_t C, void* y,
+                         efqat_stream_t stream);
+
+/* ---- layer norm ------------------------------------------------------------------------ */
+/* Over the C columns of each row of x [M,C]:  mean, rstd = 1 / sqrt(var + eps) (biased variance,
+ * formed from the centred values), y = (x - mean) * rstd * gamma + beta.  gamma, beta fp32 [C]
+ * (beta may be NULL), mean and rstd fp32 [M].  fwd also writes the checkpoint of x when
+ * save_or_null is given.  bwd, with xh = (x - mean) * rstd and g = dY * gamma:
+ *   dX = rstd * (g - mean_c(g) - xh * mean_c(g * xh)),  dgamma[c] = sum_m dY * xh,  dbeta[c] = sum_m dY
+ * from x or from its checkpoint (exactly one of the two; mean and rstd are those of x either way);
+ * the sums over rows are taken in a fixed order (the same bits every time).  Zero rows give zero
+ * dgamma and dbeta.  recompute forms y again from the checkpoint and the saved mean and rstd.
+ * x, y, dY, dX in `dtype`; C % 8 == 0 (C % 16 == 0 with a checkpoint) and C <= 16384, else
+ * EFQAT_ERR_ALIGN / EFQAT_ERR_TOO_LARGE. */
+int efqat_layer_norm_workspace_bytes(int64_t M, int64_t C, size_t* out);
+int efqat_layer_norm_fwd(efqat_ctx* ctx, int dtype, const void* x, int64_t M, int64_t C, const float* gamma,
+                         const float* beta_or_null, float eps, void* y, float* mean, float* rstd,
+                         const efqat_ckpt* save_or_null, efqat_stream_t stream);
+int efqat_layer_norm_bwd(efqat_ctx* ctx, int dtype, const void* dY, const void* x_or_null,
+                         const efqat_ckpt* saved_or_null, int64_t M, int64_t C, const float* gamma,
+                         const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta, void* ws,
+                         size_t ws_bytes, efqat_stream_t stream);
+int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* saved, int64_t M, int64_t C,
+                               const float* gamma, const float* beta_or_null, const float* mean,
+                               const float* rstd, void* y, efqat_stream_t stream);
+
 /* ---- helpers: quantizer export and MinMax initialisation ---------------------------- */
 /* Eq. 1: codes int32 [count] (asymmetric: 0..2^b-1; symmetric: signed), clip uint8 [count]
  * (0 in range, 1 clipped low, 2 clipped high), either may be NULL.  x in `dtype`. */

@@ -30,7 +30,9 @@ EXPORTS = [
     "efqat_selftest_bounded_wait", "efqat_qparam_adam", "efqat_log2_scale_init",
     "efqat_weight_cache_bytes", "efqat_weight_cache_update", "efqat_fq_linear_fwd_cached",
     "efqat_fq_linear_bwd_cached", "efqat_network_fwd", "efqat_network_bwd", "efqat_network_cache_update",
-    "efqat_network_qparam_adam",
+    "efqat_network_qparam_adam", "efqat_ckpt_bytes", "efqat_ckpt_store", "efqat_ckpt_load", "efqat_gelu_fwd",
+    "efqat_gelu_bwd", "efqat_gelu_recompute", "efqat_layer_norm_workspace_bytes", "efqat_layer_norm_fwd",
+    "efqat_layer_norm_bwd", "efqat_layer_norm_recompute",
 ]
 
 
@@ -70,6 +72,11 @@ class NetLayer(C.Structure):
                 ("opt_or_null", C.POINTER(Sgd)),
                 ("cache_or_null", C.c_void_p), ("cache_bytes", C.c_size_t),
                 ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class CkptArrays(C.Structure):
+    """efqat_ckpt: the two device arrays of an 8-bit activation checkpoint."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
 
 
 class EfqatError(RuntimeError):
@@ -128,6 +135,17 @@ def load() -> C.CDLL:
     for nm in ("efqat_network_fwd", "efqat_network_bwd", "efqat_network_cache_update"):
         getattr(lib, nm).argtypes = [vp, i32, C.POINTER(NetLayer), vp]
     lib.efqat_network_qparam_adam.argtypes = [vp, C.POINTER(Adam), i32, C.POINTER(NetLayer), C.POINTER(QParamState), vp]
+    ck = C.POINTER(CkptArrays)
+    lib.efqat_ckpt_bytes.argtypes = [i64, i64, C.POINTER(sz), C.POINTER(sz)]
+    lib.efqat_ckpt_store.argtypes = [vp, i32, vp, i64, i64, ck, vp]
+    lib.efqat_ckpt_load.argtypes = [vp, i32, ck, i64, i64, vp, vp]
+    lib.efqat_gelu_fwd.argtypes = [vp, i32, vp, i64, i64, vp, ck, vp]
+    lib.efqat_gelu_bwd.argtypes = [vp, i32, vp, vp, ck, i64, i64, vp, vp]
+    lib.efqat_gelu_recompute.argtypes = [vp, i32, ck, i64, i64, vp, vp]
+    lib.efqat_layer_norm_workspace_bytes.argtypes = [i64, i64, C.POINTER(sz)]
+    lib.efqat_layer_norm_fwd.argtypes = [vp, i32, vp, i64, i64, vp, vp, C.c_float, vp, vp, vp, ck, vp]
+    lib.efqat_layer_norm_bwd.argtypes = [vp, i32, vp, vp, ck, i64, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.efqat_layer_norm_recompute.argtypes = [vp, i32, ck, i64, i64, vp, vp, vp, vp, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("efqat_status_string", "efqat_ratio_to_k", "efqat_launch_count"):
@@ -525,6 +543,163 @@ class QParamOptimizer:
         rc = load().efqat_qparam_adam(self.ctx.handle, C.byref(self.opt), C.byref(self.state), self.N, _ptr(idx),
                                       int(k_sel), _ptr(dS_w_sel), _ptr(dS_x), _ptr(dZ_x), _stream())
         _check(rc, "efqat_qparam_adam")
+
+
+# ---------------------------------------------------------------------------------------
+# 8-bit activation checkpoints, GELU, layer norm
+def _same(t: torch.Tensor, shape, dtype) -> int:
+    """Device address of a tensor that must be a contiguous CUDA tensor of this shape and type."""
+    if t.dtype is not dtype or tuple(t.shape) != shape:
+        raise ValueError(f"expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous CUDA tensor")
+    return t.data_ptr()
+
+
+def _code(dtype: torch.dtype) -> int:
+    if dtype is torch.bfloat16:
+        return BF16
+    if dtype is torch.float32:
+        return F32
+    raise TypeError(f"activations must be fp32 or bf16, got {dtype}")
+
+
+class Checkpoint:
+    """An activation [M,C] kept in 8 bits (efqat_ckpt): int8 codes and one fp32 scale per 128 elements of a
+    row.  Written by store() or by the forward of LayerNormPlan / GeluPlan, read by load() or by their
+    backward and recompute."""
+
+    GROUP = 128
+
+    def __init__(self, ctx: Context, M: int, C_: int, device):
+        nc, ns = C.c_size_t(0), C.c_size_t(0)
+        _check(load().efqat_ckpt_bytes(int(M), int(C_), C.byref(nc), C.byref(ns)), "efqat_ckpt_bytes")
+        self.ctx, self.shape = ctx, (int(M), int(C_))
+        self.nbytes = nc.value + ns.value
+        self.codes = torch.empty(self.shape, dtype=torch.int8, device=device)
+        self.scales = torch.empty((int(M), -(-int(C_) // self.GROUP)), dtype=torch.float32, device=device)
+        self.arrays = CkptArrays(self.codes.data_ptr(), self.scales.data_ptr())
+        self.ref = C.byref(self.arrays)
+
+    def store(self, x: torch.Tensor) -> "Checkpoint":
+        """efqat_ckpt_store."""
+        rc = load().efqat_ckpt_store(self.ctx.handle, _code(x.dtype), _same(x, self.shape, x.dtype), *self.shape,
+                                     self.ref, _stream())
+        _check(rc, "efqat_ckpt_store")
+        return self
+
+    def load(self, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """efqat_ckpt_load: the activation the checkpoint stands for, in `out` or a new tensor of `dtype`."""
+        if out is None:
+            out = torch.empty(self.shape, dtype=dtype, device=self.codes.device)
+        rc = load().efqat_ckpt_load(self.ctx.handle, _code(out.dtype), self.ref, *self.shape,
+                                    _same(out, self.shape, out.dtype), _stream())
+        _check(rc, "efqat_ckpt_load")
+        return out
+
+
+def _source(x: Optional[torch.Tensor], saved: Optional[Checkpoint], shape, dtype):
+    """(address of x or None, reference to the checkpoint or None): exactly one of the two."""
+    if (x is None) == (saved is None):
+        raise ValueError("give either x or its checkpoint")
+    if saved is None:
+        return _same(x, shape, dtype), None
+    if saved.shape != shape:
+        raise ValueError(f"checkpoint of shape {saved.shape}, expected {shape}")
+    return None, saved.ref
+
+
+def _save(save: Optional[Checkpoint], shape):
+    if save is None:
+        return None
+    if save.shape != shape:
+        raise ValueError(f"checkpoint of shape {save.shape}, expected {shape}")
+    return save.ref
+
+
+class GeluPlan:
+    """GELU over [M,C] activations; the output tensors are owned and reused by the plan."""
+
+    def __init__(self, ctx: Context, M: int, C_: int, dtype: torch.dtype, device):
+        self.ctx, self.shape, self.dtype, self.code = ctx, (int(M), int(C_)), dtype, _code(dtype)
+        self.y = torch.empty(self.shape, dtype=dtype, device=device)
+        self.dx = torch.empty(self.shape, dtype=dtype, device=device)
+
+    def fwd(self, x: torch.Tensor, save: Optional[Checkpoint] = None) -> torch.Tensor:
+        """efqat_gelu_fwd: y, and the checkpoint of x in `save` when given."""
+        rc = load().efqat_gelu_fwd(self.ctx.handle, self.code, _same(x, self.shape, self.dtype), *self.shape,
+                                   self.y.data_ptr(), _save(save, self.shape), _stream())
+        _check(rc, "efqat_gelu_fwd")
+        return self.y
+
+    def bwd(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, saved: Optional[Checkpoint] = None) -> torch.Tensor:
+        """efqat_gelu_bwd: dx from dy and either x or its checkpoint."""
+        px, ps = _source(x, saved, self.shape, self.dtype)
+        rc = load().efqat_gelu_bwd(self.ctx.handle, self.code, _same(dy, self.shape, self.dtype), px, ps, *self.shape,
+                                   self.dx.data_ptr(), _stream())
+        _check(rc, "efqat_gelu_bwd")
+        return self.dx
+
+    def recompute(self, saved: Checkpoint) -> torch.Tensor:
+        """efqat_gelu_recompute: y again, from the checkpoint."""
+        rc = load().efqat_gelu_recompute(self.ctx.handle, self.code, _save(saved, self.shape), *self.shape,
+                                         self.y.data_ptr(), _stream())
+        _check(rc, "efqat_gelu_recompute")
+        return self.y
+
+
+def layer_norm_workspace_bytes(M: int, C_: int) -> int:
+    out = C.c_size_t(0)
+    _check(load().efqat_layer_norm_workspace_bytes(int(M), int(C_), C.byref(out)), "efqat_layer_norm_workspace_bytes")
+    return out.value
+
+
+class LayerNormPlan:
+    """Layer norm over the rows of [M,C] activations; outputs, statistics and workspace are owned and reused
+    by the plan (y, mean, rstd of the last forward; dx, dgamma, dbeta of the last backward)."""
+
+    def __init__(self, ctx: Context, M: int, C_: int, dtype: torch.dtype, device, eps: float = 1e-5,
+                 backward: bool = True):
+        self.ctx, self.shape, self.dtype, self.code, self.eps = ctx, (int(M), int(C_)), dtype, _code(dtype), float(eps)
+        new = lambda *shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=device)
+        self.param = (int(C_),)
+        self.y = new(*self.shape, dt=dtype)
+        self.mean, self.rstd = new(int(M)), new(int(M))
+        self.ws = alloc_workspace(layer_norm_workspace_bytes(M, C_), device)
+        if backward:
+            self.dx, self.dgamma, self.dbeta = new(*self.shape, dt=dtype), new(int(C_)), new(int(C_))
+
+    def _beta(self, beta):
+        return None if beta is None else _same(beta, self.param, torch.float32)
+
+    def fwd(self, x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None,
+            save: Optional[Checkpoint] = None) -> torch.Tensor:
+        """efqat_layer_norm_fwd: y (and self.mean, self.rstd), and the checkpoint of x in `save` when given."""
+        rc = load().efqat_layer_norm_fwd(self.ctx.handle, self.code, _same(x, self.shape, self.dtype), *self.shape,
+                                         _same(gamma, self.param, torch.float32), self._beta(beta), self.eps,
+                                         self.y.data_ptr(), self.mean.data_ptr(), self.rstd.data_ptr(),
+                                         _save(save, self.shape), _stream())
+        _check(rc, "efqat_layer_norm_fwd")
+        return self.y
+
+    def bwd(self, dy: torch.Tensor, gamma: torch.Tensor, x: Optional[torch.Tensor] = None,
+            saved: Optional[Checkpoint] = None):
+        """efqat_layer_norm_bwd with the statistics of the last forward: dict(dx, dgamma, dbeta)."""
+        px, ps = _source(x, saved, self.shape, self.dtype)
+        rc = load().efqat_layer_norm_bwd(self.ctx.handle, self.code, _same(dy, self.shape, self.dtype), px, ps,
+                                         *self.shape, _same(gamma, self.param, torch.float32), self.mean.data_ptr(),
+                                         self.rstd.data_ptr(), self.dx.data_ptr(), self.dgamma.data_ptr(),
+                                         self.dbeta.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream())
+        _check(rc, "efqat_layer_norm_bwd")
+        return dict(dx=self.dx, dgamma=self.dgamma, dbeta=self.dbeta)
+
+    def recompute(self, saved: Checkpoint, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """efqat_layer_norm_recompute: y again, from the checkpoint and the statistics of the last forward."""
+        rc = load().efqat_layer_norm_recompute(self.ctx.handle, self.code, _save(saved, self.shape), *self.shape,
+                                               _same(gamma, self.param, torch.float32), self._beta(beta),
+                                               self.mean.data_ptr(), self.rstd.data_ptr(), self.y.data_ptr(), _stream())
+        _check(rc, "efqat_layer_norm_recompute")
+        return self.y
 
 
 def fake_quant_act(ctx: Context, x, s_x, z_x, x_bits=8, x_symmetric=False):

@@ -1,11 +1,13 @@
 // C ABI of the library: argument validation, workspace carving and the launch sequence
 // of each entry point.  Every step of the path runs in this library's kernels; there is
 // no host fallback.
+#include <initializer_list>
 #include <new>
 #include <vector>
 
 #include "../../include/efqat_aux.h"
 #include "internal.h"
+#include "rowops.cuh"
 
 using namespace efqat;
 
@@ -289,6 +291,17 @@ WCache carve_cache(void* cache, const efqat_layer_desc* l) {
   return c;
 }
 
+// SM count of the current CUDA device (148, a B200, where no device can be asked): the workspace
+// queries have no context, but the compute calls require their context's device to be current.
+int current_sm_count() {
+  int dev = -1, n = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 &&
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0)
+    return n;
+  cudaGetLastError();
+  return 148;
+}
+
 int guard_device(const efqat_ctx* ctx) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess || dev != ctx->device) return EFQAT_ERR_CUDA;
@@ -447,12 +460,7 @@ int efqat_workspace_bytes(const efqat_layer_desc* layer, const efqat_qspec* q, i
   // (fewer channels -> more splits of the contraction); take its maximum.  The split rule
   // depends on the SM count: that of the current CUDA device, the one the compute calls
   // require to be current as well (148, a B200, where no device can be asked).
-  int sm = 148, dev = -1, n = 0;
-  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 &&
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0)
-    sm = n;
-  else
-    cudaGetLastError();
+  const int sm = current_sm_count();
   int64_t p_max = 0;
   for (int64_t k = 1; k <= k_sel_max; ++k) {
     const int64_t nc = (k < layer->N) ? round_up(k, 16) : layer->N;
@@ -1026,6 +1034,158 @@ int efqat_log2_scale_init(efqat_ctx* ctx, const float* s, float* theta, int64_t 
   if (rc != EFQAT_OK) return rc;
   Entered in(ctx);
   launch_log2_init(s, theta, n, ctx->d_status, stream);
+  return last_error();
+}
+
+// ---- activation checkpoints, GELU, layer norm ---------------------------------------------
+// Row kernels shared checks: `unit` = required divisor of C (16 with a checkpoint, else 8).
+static int check_rows(efqat_ctx* ctx, int dtype, int64_t M, int64_t C, const efqat_ckpt* ck) {
+  if (!ctx) return EFQAT_ERR_NULL;
+  if (dtype != EFQAT_F32 && dtype != EFQAT_BF16) return EFQAT_ERR_DTYPE;
+  if (M < 0 || C < 1 || M > INT32_MAX || C > INT32_MAX) return EFQAT_ERR_SHAPE;
+  if (C & (ck ? 15 : 7)) return EFQAT_ERR_ALIGN;
+  if (M * ckpt_groups(C) > INT32_MAX) return EFQAT_ERR_TOO_LARGE;
+  if (ck && M > 0) {
+    if (!ck->codes || !ck->scales) return EFQAT_ERR_NULL;
+    if (!aligned16(ck->codes)) return EFQAT_ERR_ALIGN;
+  }
+  return guard_device(ctx);
+}
+
+// Required tensors of a call on M > 0 rows: present and 16-byte aligned.
+static int check_tensors(int64_t M, std::initializer_list<const void*> ts) {
+  if (M == 0) return EFQAT_OK;
+  for (const void* t : ts) {
+    if (!t) return EFQAT_ERR_NULL;
+    if (!aligned16(t)) return EFQAT_ERR_ALIGN;
+  }
+  return EFQAT_OK;
+}
+
+int efqat_ckpt_bytes(int64_t M, int64_t C, size_t* codes_bytes, size_t* scales_bytes) {
+  if (!codes_bytes || !scales_bytes) return EFQAT_ERR_NULL;
+  if (M < 0 || C < 1 || M > INT32_MAX || C > INT32_MAX) return EFQAT_ERR_SHAPE;
+  if (C & 15) return EFQAT_ERR_ALIGN;
+  if (M * ckpt_groups(C) > INT32_MAX) return EFQAT_ERR_TOO_LARGE;
+  *codes_bytes = static_cast<size_t>(M) * C;
+  *scales_bytes = static_cast<size_t>(M) * ckpt_groups(C) * sizeof(float);
+  return EFQAT_OK;
+}
+
+// act: see launch_ckpt.  The caller has checked its own arguments except the tensors.
+static int rows_impl(efqat_ctx* ctx, int dtype, int act, const void* x, const efqat_ckpt* in, const void* dY, int64_t M,
+                     int64_t C, void* y, const efqat_ckpt* out, efqat_stream_t stream) {
+  if (M == 0) return EFQAT_OK;
+  Entered guard(ctx);
+  launch_ckpt(dtype, act, x, in, dY, M, C, y, out, ctx->sm_count, stream);
+  return last_error();
+}
+
+int efqat_ckpt_store(efqat_ctx* ctx, int dtype, const void* x, int64_t M, int64_t C, const efqat_ckpt* out,
+                     efqat_stream_t stream) {
+  if (!out) return EFQAT_ERR_NULL;
+  int rc = check_rows(ctx, dtype, M, C, out);
+  if (rc == EFQAT_OK) rc = check_tensors(M, {x});
+  return rc != EFQAT_OK ? rc : rows_impl(ctx, dtype, 0, x, nullptr, nullptr, M, C, nullptr, out, stream);
+}
+
+int efqat_ckpt_load(efqat_ctx* ctx, int dtype, const efqat_ckpt* in, int64_t M, int64_t C, void* x,
+                    efqat_stream_t stream) {
+  if (!in) return EFQAT_ERR_NULL;
+  int rc = check_rows(ctx, dtype, M, C, in);
+  if (rc == EFQAT_OK) rc = check_tensors(M, {x});
+  return rc != EFQAT_OK ? rc : rows_impl(ctx, dtype, 0, nullptr, in, nullptr, M, C, x, nullptr, stream);
+}
+
+int efqat_gelu_fwd(efqat_ctx* ctx, int dtype, const void* x, int64_t M, int64_t C, void* y,
+                   const efqat_ckpt* save_or_null, efqat_stream_t stream) {
+  int rc = check_rows(ctx, dtype, M, C, save_or_null);
+  if (rc == EFQAT_OK) rc = check_tensors(M, {x, y});
+  return rc != EFQAT_OK ? rc : rows_impl(ctx, dtype, 1, x, nullptr, nullptr, M, C, y, save_or_null, stream);
+}
+
+int efqat_gelu_bwd(efqat_ctx* ctx, int dtype, const void* dY, const void* x_or_null, const efqat_ckpt* saved_or_null,
+                   int64_t M, int64_t C, void* dX, efqat_stream_t stream) {
+  int rc = check_rows(ctx, dtype, M, C, saved_or_null);
+  if (rc == EFQAT_OK && x_or_null && saved_or_null) rc = EFQAT_ERR_MODE;
+  if (rc == EFQAT_OK) rc = check_tensors(M, {dY, dX});
+  if (rc == EFQAT_OK && !saved_or_null) rc = check_tensors(M, {x_or_null});
+  return rc != EFQAT_OK ? rc : rows_impl(ctx, dtype, 2, x_or_null, saved_or_null, dY, M, C, dX, nullptr, stream);
+}
+
+int efqat_gelu_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* saved, int64_t M, int64_t C, void* y,
+                         efqat_stream_t stream) {
+  if (!saved) return EFQAT_ERR_NULL;
+  int rc = check_rows(ctx, dtype, M, C, saved);
+  if (rc == EFQAT_OK) rc = check_tensors(M, {y});
+  return rc != EFQAT_OK ? rc : rows_impl(ctx, dtype, 1, nullptr, saved, nullptr, M, C, y, nullptr, stream);
+}
+
+static const int64_t NORM_MAX_C = 16384;
+
+int efqat_layer_norm_workspace_bytes(int64_t M, int64_t C, size_t* out) {
+  if (!out) return EFQAT_ERR_NULL;
+  if (M < 0 || C < 1 || M > INT32_MAX) return EFQAT_ERR_SHAPE;
+  if (C & 7) return EFQAT_ERR_ALIGN;
+  if (C > NORM_MAX_C) return EFQAT_ERR_TOO_LARGE;
+  *out = layer_norm_workspace_bytes(M, C, current_sm_count()) + 256;
+  return EFQAT_OK;
+}
+
+int efqat_layer_norm_fwd(efqat_ctx* ctx, int dtype, const void* x, int64_t M, int64_t C, const float* gamma,
+                         const float* beta_or_null, float eps, void* y, float* mean, float* rstd,
+                         const efqat_ckpt* save_or_null, efqat_stream_t stream) {
+  int rc = check_rows(ctx, dtype, M, C, save_or_null);
+  if (rc == EFQAT_OK && C > NORM_MAX_C) rc = EFQAT_ERR_TOO_LARGE;
+  if (rc == EFQAT_OK && !(eps >= 0.f && isfinite(eps))) rc = EFQAT_ERR_SHAPE;
+  if (rc == EFQAT_OK) rc = check_tensors(M, {x, y, gamma});
+  if (rc == EFQAT_OK && beta_or_null) rc = check_tensors(M, {beta_or_null});
+  if (rc == EFQAT_OK && M > 0 && (!mean || !rstd)) rc = EFQAT_ERR_NULL;
+  if (rc != EFQAT_OK || M == 0) return rc;
+  Entered in(ctx);
+  launch_norm_fwd(dtype, x, nullptr, M, C, gamma, beta_or_null, eps, y, mean, rstd, save_or_null, ctx->sm_count, stream);
+  return last_error();
+}
+
+int efqat_layer_norm_bwd(efqat_ctx* ctx, int dtype, const void* dY, const void* x_or_null,
+                         const efqat_ckpt* saved_or_null, int64_t M, int64_t C, const float* gamma, const float* mean,
+                         const float* rstd, void* dX, float* dgamma, float* dbeta, void* ws, size_t ws_bytes,
+                         efqat_stream_t stream) {
+  int rc = check_rows(ctx, dtype, M, C, saved_or_null);
+  if (rc == EFQAT_OK && C > NORM_MAX_C) rc = EFQAT_ERR_TOO_LARGE;
+  if (rc == EFQAT_OK && x_or_null && saved_or_null) rc = EFQAT_ERR_MODE;
+  if (rc == EFQAT_OK && (!dgamma || !dbeta)) rc = EFQAT_ERR_NULL;
+  if (rc == EFQAT_OK) rc = check_tensors(M, {dY, dX, gamma});
+  if (rc == EFQAT_OK && !saved_or_null) rc = check_tensors(M, {x_or_null});
+  if (rc == EFQAT_OK && M > 0 && (!mean || !rstd)) rc = EFQAT_ERR_NULL;
+  if (rc != EFQAT_OK) return rc;
+  if (M == 0) {
+    if (cudaMemsetAsync(dgamma, 0, C * sizeof(float), stream) != cudaSuccess ||
+        cudaMemsetAsync(dbeta, 0, C * sizeof(float), stream) != cudaSuccess)
+      return EFQAT_ERR_CUDA;
+    return EFQAT_OK;
+  }
+  if (!ws || ws_bytes < layer_norm_workspace_bytes(M, C, ctx->sm_count) + 256) return EFQAT_ERR_WORKSPACE;
+  Entered in(ctx);
+  float* part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255));
+  launch_norm_bwd(dtype, dY, x_or_null, saved_or_null, M, C, gamma, mean, rstd, dX, dgamma, dbeta, part, ctx->sm_count,
+                  stream);
+  return last_error();
+}
+
+int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* saved, int64_t M, int64_t C,
+                               const float* gamma, const float* beta_or_null, const float* mean, const float* rstd,
+                               void* y, efqat_stream_t stream) {
+  if (!saved) return EFQAT_ERR_NULL;
+  int rc = check_rows(ctx, dtype, M, C, saved);
+  if (rc == EFQAT_OK && C > NORM_MAX_C) rc = EFQAT_ERR_TOO_LARGE;
+  if (rc == EFQAT_OK) rc = check_tensors(M, {y, gamma});
+  if (rc == EFQAT_OK && beta_or_null) rc = check_tensors(M, {beta_or_null});
+  if (rc == EFQAT_OK && M > 0 && (!mean || !rstd)) rc = EFQAT_ERR_NULL;
+  if (rc != EFQAT_OK || M == 0) return rc;
+  Entered in(ctx);
+  launch_norm_fwd(dtype, nullptr, saved, M, C, gamma, beta_or_null, 0.f, y, const_cast<float*>(mean),
+                  const_cast<float*>(rstd), nullptr, ctx->sm_count, stream);
   return last_error();
 }
 

@@ -104,6 +104,23 @@ void launch_qparam_adam(const efqat_adam& a, const efqat_qparam_state& st, int64
                         cudaStream_t stream);
 void launch_log2_init(const float* s, float* theta, int64_t n, int* status, cudaStream_t stream);
 
+// ---- ckpt.cu ------------------------------------------------------------------------
+// One streaming pass over [M,C].  act: 0 none (x given: store into `out`; `in` given: load into y),
+// 1 GELU (optionally also storing x into `out`), 2 GELU backward (dy).  Exactly one of x, in.
+void launch_ckpt(int dtype, int act, const void* x, const efqat_ckpt* in, const void* dy, int64_t M, int64_t C,
+                 void* y, const efqat_ckpt* out, int sm_count, cudaStream_t st);
+
+// ---- norm.cu ------------------------------------------------------------------------
+// in given: y from the checkpoint and the given mean / rstd; else mean and rstd are written.
+void launch_norm_fwd(int dtype, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
+                     const float* beta, float eps, void* y, float* mean, float* rstd, const efqat_ckpt* out,
+                     int sm_count, cudaStream_t st);
+// part: layer_norm_workspace_bytes() of partial sums.
+void launch_norm_bwd(int dtype, const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C,
+                     const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta,
+                     float* part, int sm_count, cudaStream_t st);
+size_t layer_norm_workspace_bytes(int64_t M, int64_t C, int sm_count);
+
 // ---- cache.cu -----------------------------------------------------------------------
 // Rebuilds rows of a layer's weight-operand cache: rows idx[0..rows) (idx null: rows 0..rows).
 // codes8 + wsum (integer forward) or codes16 (bf16 forward) and what (backward) as laid out

@@ -154,3 +154,22 @@ def test_network_layer_lists():
     by = {c.name: c for c in r50}
     assert by["rn50_s2b1_b"].H == 56 and by["rn50_s2b1_b"].stride == 2 and by["rn50_s2b1_c"].H == 28
     assert by["rn50_s4b3_c"].H == 7 and by["rn50_s4b3_c"].N == 2048
+
+
+def test_row_operator_queries(lib):
+    """Sizes of checkpoints and of the layer-norm workspace, and the refusals of the queries."""
+    nc, ns = C.c_size_t(0), C.c_size_t(0)
+    assert lib.efqat_ckpt_bytes(9216, 1040, C.byref(nc), C.byref(ns)) == 0
+    assert (nc.value, ns.value) == (9216 * 1040, 9216 * 9 * 4)
+    assert lib.efqat_ckpt_bytes(0, 16, C.byref(nc), C.byref(ns)) == 0 and nc.value == 0
+    assert lib.efqat_ckpt_bytes(4, 24, C.byref(nc), C.byref(ns)) == -3
+    assert lib.efqat_ckpt_bytes(-1, 16, C.byref(nc), C.byref(ns)) == -2
+    assert lib.efqat_ckpt_bytes(4, 16, None, C.byref(ns)) == -1
+    assert lib.efqat_ckpt_bytes(2 ** 31 - 1, 2 ** 20, C.byref(nc), C.byref(ns)) == -11
+    assert B.layer_norm_workspace_bytes(1, 768) >= 2 * 768 * 4
+    for args, code in (((4, 100), -3), ((4, 16392), -11), ((-1, 8), -2)):
+        with pytest.raises(B.EfqatError) as e:
+            B.layer_norm_workspace_bytes(*args)
+        assert e.value.code == code
+    assert lib.efqat_gelu_fwd(None, 1, None, 4, 16, None, None, None) == -1
+    assert lib.efqat_layer_norm_fwd(None, 1, None, 4, 16, None, None, 1e-5, None, None, None, None, None) == -1
