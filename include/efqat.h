@@ -316,6 +316,27 @@ int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* save
                                const float* gamma, const float* beta_or_null, const float* mean,
                                const float* rstd, void* y, efqat_stream_t stream);
 
+/* ---- language-model loss: softmax cross entropy over a large vocabulary ------------------ */
+/* H bf16 [T,D] hidden states, W bf16 [V,D] output matrix, labels int32 [T]; logits l = H W^T are
+ * formed in pieces of the vocabulary with fp32 accumulation and never stored:
+ *   lse[t] = log sum_v exp l[t,v],   loss[t] = lse[t] - l[t,label]            (fp32 [T])
+ * A token with a negative label has no target: its loss is 0 (its lse is formed all the same) and
+ * it takes no part in the backward, whatever its hidden state holds.  A label >= V counts as none
+ * and is reported as EFQAT_DEV_BAD_INDEX.
+ * bwd: with dloss fp32 [T] (the gradient of the caller's scalar with respect to loss[t]) and
+ *   G[t,v] = dloss[t] * (exp(l[t,v] - lse[t]) - [v = label])
+ *   dH = G W  bf16 [T,D],   dW = G^T H  bf16 [V,D]   (both written whole; fixed order of all sums).
+ * G / max|dloss| is rounded to bf16 as the operand of the two products; sums are fp32, dH and dW
+ * are rounded once.  V and T may be any size (T = 0: dW is zeroed), D % 8 == 0; T, V <= 2^24 and
+ * D <= 2^20.  The workspace of the backward holds one piece of G, at most about 256 MiB, a copy of
+ * the hidden states that have a target and fp32 sums of dH. */
+int efqat_lm_loss_workspace_bytes(int64_t T, int64_t V, int64_t D, size_t* fwd_bytes, size_t* bwd_bytes);
+int efqat_lm_loss_fwd(efqat_ctx* ctx, const void* H, const void* W, const int32_t* labels, int64_t T, int64_t V,
+                      int64_t D, float* loss, float* lse, void* ws, size_t ws_bytes, efqat_stream_t stream);
+int efqat_lm_loss_bwd(efqat_ctx* ctx, const void* H, const void* W, const int32_t* labels, const float* lse,
+                      const float* dloss, int64_t T, int64_t V, int64_t D, void* dH, void* dW, void* ws,
+                      size_t ws_bytes, efqat_stream_t stream);
+
 /* ---- helpers: quantizer export and MinMax initialisation ---------------------------- */
 /* Eq. 1: codes int32 [count] (asymmetric: 0..2^b-1; symmetric: signed), clip uint8 [count]
  * (0 in range, 1 clipped low, 2 clipped high), either may be NULL.  x in `dtype`. */

@@ -32,7 +32,8 @@ EXPORTS = [
     "efqat_fq_linear_bwd_cached", "efqat_network_fwd", "efqat_network_bwd", "efqat_network_cache_update",
     "efqat_network_qparam_adam", "efqat_ckpt_bytes", "efqat_ckpt_store", "efqat_ckpt_load", "efqat_gelu_fwd",
     "efqat_gelu_bwd", "efqat_gelu_recompute", "efqat_layer_norm_workspace_bytes", "efqat_layer_norm_fwd",
-    "efqat_layer_norm_bwd", "efqat_layer_norm_recompute",
+    "efqat_layer_norm_bwd", "efqat_layer_norm_recompute", "efqat_lm_loss_workspace_bytes", "efqat_lm_loss_fwd",
+    "efqat_lm_loss_bwd",
 ]
 
 
@@ -146,6 +147,9 @@ def load() -> C.CDLL:
     lib.efqat_layer_norm_fwd.argtypes = [vp, i32, vp, i64, i64, vp, vp, C.c_float, vp, vp, vp, ck, vp]
     lib.efqat_layer_norm_bwd.argtypes = [vp, i32, vp, vp, ck, i64, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.efqat_layer_norm_recompute.argtypes = [vp, i32, ck, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.efqat_lm_loss_workspace_bytes.argtypes = [i64, i64, i64, C.POINTER(sz), C.POINTER(sz)]
+    lib.efqat_lm_loss_fwd.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
+    lib.efqat_lm_loss_bwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("efqat_status_string", "efqat_ratio_to_k", "efqat_launch_count"):
@@ -700,6 +704,48 @@ class LayerNormPlan:
                                                self.mean.data_ptr(), self.rstd.data_ptr(), self.y.data_ptr(), _stream())
         _check(rc, "efqat_layer_norm_recompute")
         return self.y
+
+
+def lm_loss_workspace_bytes(T: int, V: int, D: int):
+    """(bytes of the forward's workspace, bytes of the backward's)."""
+    fwd, bwd = C.c_size_t(0), C.c_size_t(0)
+    _check(load().efqat_lm_loss_workspace_bytes(int(T), int(V), int(D), C.byref(fwd), C.byref(bwd)),
+           "efqat_lm_loss_workspace_bytes")
+    return fwd.value, bwd.value
+
+
+class LmLossPlan:
+    """Softmax cross entropy of T tokens over a vocabulary of V, hidden size D (efqat_lm_loss_fwd / _bwd); the
+    outputs and the workspace are owned and reused by the plan (lse of the last forward feeds its backward)."""
+
+    def __init__(self, ctx: Context, T: int, V: int, D: int, device, backward: bool = True):
+        self.ctx, self.dims = ctx, (int(T), int(V), int(D))
+        self.h_shape, self.w_shape, self.t_shape = (int(T), int(D)), (int(V), int(D)), (int(T),)
+        fwd, bwd = lm_loss_workspace_bytes(T, V, D)
+        new = lambda shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=device)
+        self.loss, self.lse = new(self.t_shape), new(self.t_shape)
+        self.ws = alloc_workspace(max(fwd, bwd if backward else 0), device)
+        if backward:
+            self.dH, self.dW = new(self.h_shape, torch.bfloat16), new(self.w_shape, torch.bfloat16)
+
+    def fwd(self, H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
+        """efqat_lm_loss_fwd: the loss of each token, 0 where the label is negative (and self.lse)."""
+        rc = load().efqat_lm_loss_fwd(self.ctx.handle, _same(H, self.h_shape, torch.bfloat16),
+                                      _same(W, self.w_shape, torch.bfloat16), _same(labels, self.t_shape, torch.int32),
+                                      *self.dims, self.loss.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(),
+                                      self.ws.numel(), _stream())
+        _check(rc, "efqat_lm_loss_fwd")
+        return self.loss
+
+    def bwd(self, H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, dloss: torch.Tensor):
+        """efqat_lm_loss_bwd with the lse of the last forward: dict(dH, dW)."""
+        rc = load().efqat_lm_loss_bwd(self.ctx.handle, _same(H, self.h_shape, torch.bfloat16),
+                                      _same(W, self.w_shape, torch.bfloat16), _same(labels, self.t_shape, torch.int32),
+                                      self.lse.data_ptr(), _same(dloss, self.t_shape, torch.float32), *self.dims,
+                                      self.dH.data_ptr(), self.dW.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
+                                      _stream())
+        _check(rc, "efqat_lm_loss_bwd")
+        return dict(dH=self.dH, dW=self.dW)
 
 
 def fake_quant_act(ctx: Context, x, s_x, z_x, x_bits=8, x_symmetric=False):

@@ -347,6 +347,7 @@ int efqat_create(efqat_ctx** out, int device) {
       cudaMalloc(&c->d_status, 256) != cudaSuccess || cudaMemset(c->d_status, 0, 256) != cudaSuccess)
     rc = EFQAT_ERR_CUDA;
   if (rc == EFQAT_OK) rc = gemm_init();
+  if (rc == EFQAT_OK) rc = lm_loss_init();
   cudaSetDevice(prev);
   if (rc != EFQAT_OK) {
     delete c;
@@ -1187,6 +1188,63 @@ int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* save
   launch_norm_fwd(dtype, nullptr, saved, M, C, gamma, beta_or_null, 0.f, y, const_cast<float*>(mean),
                   const_cast<float*>(rstd), nullptr, ctx->sm_count, stream);
   return last_error();
+}
+
+// ---- language-model loss --------------------------------------------------------------------
+static int check_lm(int64_t T, int64_t V, int64_t D) {
+  if (T < 0 || V < 1 || D < 1) return EFQAT_ERR_SHAPE;
+  if (D & 7) return EFQAT_ERR_ALIGN;
+  // row and column numbers of every matrix, and of the fp32 partial sums, stay within 2^30
+  if (T > (1 << 24) || V > (1 << 24) || D > (1 << 20)) return EFQAT_ERR_TOO_LARGE;
+  return EFQAT_OK;
+}
+
+int efqat_lm_loss_workspace_bytes(int64_t T, int64_t V, int64_t D, size_t* fwd_bytes, size_t* bwd_bytes) {
+  if (!fwd_bytes || !bwd_bytes) return EFQAT_ERR_NULL;
+  const int rc = check_lm(T, V, D);
+  if (rc != EFQAT_OK) return rc;
+  *fwd_bytes = *bwd_bytes = 0;
+  if (T > 0) lm_loss_workspace_bytes(T, V, D, current_sm_count(), fwd_bytes, bwd_bytes);
+  return EFQAT_OK;
+}
+
+int efqat_lm_loss_fwd(efqat_ctx* ctx, const void* H, const void* W, const int32_t* labels, int64_t T, int64_t V,
+                      int64_t D, float* loss, float* lse, void* ws, size_t ws_bytes, efqat_stream_t stream) {
+  if (!ctx) return EFQAT_ERR_NULL;
+  int rc = check_lm(T, V, D);
+  if (rc == EFQAT_OK) rc = check_tensors(T, {H, W});
+  if (rc == EFQAT_OK && T > 0 && (!labels || !loss || !lse)) rc = EFQAT_ERR_NULL;
+  if (rc == EFQAT_OK) rc = guard_device(ctx);
+  if (rc != EFQAT_OK || T == 0) return rc;
+  size_t need = 0, other = 0;
+  lm_loss_workspace_bytes(T, V, D, ctx->sm_count, &need, &other);
+  if (!ws || ws_bytes < need) return EFQAT_ERR_WORKSPACE;
+  Entered in(ctx);
+  rc = run_lm_loss_fwd(static_cast<const bf16*>(H), static_cast<const bf16*>(W), labels, T, V, D, loss, lse, ws,
+                       ctx->d_status, ctx->sm_count, stream);
+  return rc != EFQAT_OK ? rc : last_error();
+}
+
+int efqat_lm_loss_bwd(efqat_ctx* ctx, const void* H, const void* W, const int32_t* labels, const float* lse,
+                      const float* dloss, int64_t T, int64_t V, int64_t D, void* dH, void* dW, void* ws,
+                      size_t ws_bytes, efqat_stream_t stream) {
+  if (!ctx || !dW) return EFQAT_ERR_NULL;
+  int rc = check_lm(T, V, D);
+  if (rc == EFQAT_OK) rc = check_tensors(T, {H, W, dH});
+  if (rc == EFQAT_OK && !aligned16(dW)) rc = EFQAT_ERR_ALIGN;
+  if (rc == EFQAT_OK && T > 0 && (!labels || !lse || !dloss)) rc = EFQAT_ERR_NULL;
+  if (rc == EFQAT_OK) rc = guard_device(ctx);
+  if (rc != EFQAT_OK) return rc;
+  if (T == 0)
+    return cudaMemsetAsync(dW, 0, static_cast<size_t>(V) * D * sizeof(bf16), stream) == cudaSuccess ? EFQAT_OK
+                                                                                                     : EFQAT_ERR_CUDA;
+  size_t need = 0, other = 0;
+  lm_loss_workspace_bytes(T, V, D, ctx->sm_count, &other, &need);
+  if (!ws || ws_bytes < need) return EFQAT_ERR_WORKSPACE;
+  Entered in(ctx);
+  rc = run_lm_loss_bwd(static_cast<const bf16*>(H), static_cast<const bf16*>(W), labels, lse, dloss, T, V, D,
+                       static_cast<bf16*>(dH), static_cast<bf16*>(dW), ws, ctx->d_status, ctx->sm_count, stream);
+  return rc != EFQAT_OK ? rc : last_error();
 }
 
 int efqat_fake_quant_act(efqat_ctx* ctx, const efqat_qspec* q, int dtype, const void* x, int64_t count,

@@ -121,6 +121,16 @@ void launch_norm_bwd(int dtype, const void* dy, const void* x, const efqat_ckpt*
                      float* part, int sm_count, cudaStream_t st);
 size_t layer_norm_workspace_bytes(int64_t M, int64_t C, int sm_count);
 
+// ---- lmloss.cu ----------------------------------------------------------------------
+// Per device, with that device current (efqat_create).
+int lm_loss_init();
+void lm_loss_workspace_bytes(int64_t T, int64_t V, int64_t D, int sm_count, size_t* fwd, size_t* bwd);
+int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t T, int64_t V, int64_t D, float* loss,
+                    float* lse, void* ws, int* status, int sm_count, cudaStream_t st);
+int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const float* lse, const float* dloss,
+                    int64_t T, int64_t V, int64_t D, bf16* dH, bf16* dW, void* ws, int* status, int sm_count,
+                    cudaStream_t st);
+
 // ---- cache.cu -----------------------------------------------------------------------
 // Rebuilds rows of a layer's weight-operand cache: rows idx[0..rows) (idx null: rows 0..rows).
 // codes8 + wsum (integer forward) or codes16 (bf16 forward) and what (backward) as laid out

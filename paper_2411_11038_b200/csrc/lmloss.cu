@@ -1,0 +1,837 @@
+// Softmax cross entropy of a language-model head, in pieces of the vocabulary and without keeping
+// the logits, with its gradients.
+//
+//   l = H W^T            lse_t = log sum_v exp l_tv            loss_t = lse_t - l_t,label(t)
+//   G_tv = d_t (exp(l_tv - lse_t) - [v = label(t)])            dH = G W            dW = G^T H
+//
+// Everything heavy is one of four matrix products on the tensor cores; what follows a product
+// happens on its accumulator in the epilogue, so a logit never leaves the SM:
+//   STAT  l = H W^T     -> per row and half tile the running maximum and sum of exponentials
+//   GRAD  l = H Wc^T    -> G of one piece of the vocabulary, rounded to bf16 (an operand)
+//   DH    G Wc          -> added to fp32 sums of dH (bulk reductions in L2; one add per piece, in
+//                          stream order, so the sums have a fixed order)
+//   DW    G^T H         -> rows of dW
+// The logits of the backward are formed a second time from the stored lse: 2 of its 6 TVD
+// multiply-adds, instead of T V values kept from the forward.
+//
+// G holds p - [v = label] times d_t / max|d|: the common factor max|d| is applied in fp32 behind the
+// products, so that the mean's 1 / n, the same for every token, costs no rounding.  Tokens without a
+// target (label < 0) are left out of the backward altogether: the tokens with one are gathered to
+// the front first, and the number of them, known on the device only, sets the tiles that run.
+//
+// Kernel structure: persistent, one CTA per SM (or one pair of CTAs per two SMs, 256-row tiles),
+// warp 0 = TMA producer over a ring of stages, warp 1 = tcgen05.mma issuer and TMEM owner,
+// warps 2..9 = epilogue (TMEM lane quarter x column half) on the other one of two accumulators.
+// A token is a row, i.e. a TMEM lane, i.e. a thread: the softmax statistics need no shuffle.
+#include "internal.h"
+#include "ptx.cuh"
+
+namespace efqat {
+
+using namespace ptx;
+
+namespace {
+
+enum { LM_STAT = 0, LM_GRAD = 1, LM_DH = 2, LM_DW = 3 };
+
+static const int ROWS = 128;                    // rows of a CTA's tile = TMEM lanes
+static const int KB = 64;                       // contraction elements per k-block (one 128-byte swizzle row)
+static const int MAX_RING = 8;
+static const int A_KB_BYTES = ROWS * KB * 2;    // one k-block of the row operand
+static const int CHUNK = 64 * KB * 2;           // one 64-wide chunk of an MN-major operand
+static const int WORKERS = 8;                   // epilogue warps
+static const int THREADS = 64 + 32 * WORKERS;
+static const int ACC_COLS = 256, TMEM_ALL = 512;
+static const int STG_BYTES = 32 * 64;           // staging block of one epilogue warp: 32 rows x 64 bytes
+static const float LOG2E = 1.4426950408889634f;
+
+// What the epilogues need to know of a token with a target.
+struct __align__(16) TokenRow {
+  float nlse2;      // -lse * log2(e)
+  float ratio;      // d_t / max|d|
+  int label;
+  int pad;
+};
+
+struct LmParams {
+  int64_t Mr, Nc;             // rows (upper bound when n_rows is set) and columns of the product
+  const int* n_rows;          // number of tokens with a target: rows of STAT... GRAD, DH; contraction of DW (null: Mr)
+  int nkb;                    // k-blocks (DW with n_rows: upper bound)
+  int BN, kps, stages, splits;
+  int panel;                  // tile columns walked row block by row block (order of the work list)
+  int b_kb_bytes;
+  // STAT
+  const int32_t* labels;
+  float2* part; float* label_logit; int64_t part_pitch;
+  // GRAD
+  const TokenRow* rows; int v0;
+  // DH
+  int first; int64_t slab_rows;
+  // DW
+  const float* scale;
+  int* status;
+};
+
+struct __align__(16) Ctl {
+  uint64_t full[MAX_RING], empty[MAX_RING], acc_full[2], acc_empty[2], drain;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// 16-byte piece `piece` of row `row` of a 64-byte-swizzled staging block.
+__device__ __forceinline__ uint8_t* stg_addr(uint8_t* base, int row, int piece) {
+  return base + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4);
+}
+
+// Tile t of the work list: panels of `panel` tile columns; inside a panel row block by row block.
+// A panel's slice of the column operand stays in L2 while the row operand passes once per panel.
+__device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int panel, int& tm, int& tn) {
+  const int per = tiles_m * panel;
+  const int pn = t / per, r = t - pn * per, first = pn * panel;
+  const int width = tiles_n - first < panel ? tiles_n - first : panel;
+  tm = r / width;
+  tn = first + (r - tm * width);
+}
+
+template <int A_MN, int B_MN, int EPI, int PAIR>
+__global__ void __launch_bounds__(THREADS, 1)
+lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+          const __grid_constant__ CUtensorMap tmOut, const LmParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int a_bytes = p.kps * A_KB_BYTES, b_bytes = p.kps * p.b_kb_bytes, stage_bytes = a_bytes + b_bytes;
+  uint8_t* stg = smem + p.stages * stage_bytes;
+  Ctl* ctl = reinterpret_cast<Ctl*>(stg + (EPI == LM_STAT ? 0 : WORKERS * 2 * STG_BYTES));
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
+  const int unit = PAIR ? (blockIdx.x >> 1) : blockIdx.x;
+  const int units = PAIR ? (gridDim.x >> 1) : gridDim.x;
+  constexpr int TILE_M = PAIR ? 2 * ROWS : ROWS;
+  const int bn_cta = PAIR ? (p.BN >> 1) : p.BN;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->acc_full[b], 1);
+      mbar_init(&ctl->acc_empty[b], (PAIR ? 2 : 1) * WORKERS);
+    }
+    mbar_init(&ctl->drain, 1);
+    ctl->abort_flag = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmA);
+    prefetch_tmap(&tmB);
+    if (EPI != LM_STAT) prefetch_tmap(&tmOut);
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      tmem_alloc_pair(&ctl->tmem_base, TMEM_ALL);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(&ctl->tmem_base, TMEM_ALL);
+      tmem_relinquish();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync();      // the peer's barriers are initialised before anyone signals them
+  tc_fence_after();
+  const uint32_t tmem_base = ctl->tmem_base;
+  pdl_wait();
+  pdl_trigger();
+  volatile int* abort_flag = &ctl->abort_flag;
+
+  // The tokens with a target (at least one tile or k-block of them runs, on zeros if there are none).
+  const int n_live = p.n_rows ? *p.n_rows : static_cast<int>(EPI == LM_DW ? 0 : p.Mr);
+  const int n_run = n_live > 0 ? n_live : 1;
+  const int tiles_m = static_cast<int>(((EPI == LM_DW ? p.Mr : static_cast<int64_t>(n_run)) + TILE_M - 1) / TILE_M);
+  const int tiles_n = static_cast<int>((p.Nc + p.BN - 1) / p.BN);
+  const int nkb = EPI == LM_DW ? (n_run + KB - 1) / KB : p.nkb;
+  const int tiles = tiles_m * tiles_n, items = tiles * p.splits;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------- TMA producer
+    // Lane 0 runs the barrier protocol; lanes 0-1 / 2-5 issue the 64-wide chunks of MN-major
+    // operands (all k-blocks of a stage in one box), lanes 8.. the K-major k-blocks, A and B in turn.
+    int it = 0, s = 0;
+    uint32_t ph = 0;
+    bool live = true;
+    for (int w = unit; w < items && live; w += units) {
+      const int split = w / tiles;
+      int tm, tn;
+      tile_at(w - split * tiles, tiles_m, tiles_n, p.panel, tm, tn);
+      const int m0 = tm * TILE_M + rank * ROWS, n0 = tn * p.BN + rank * bn_cta;
+      const int kb0 = static_cast<int>(static_cast<int64_t>(split) * nkb / p.splits);
+      const int kb1 = static_cast<int>(static_cast<int64_t>(split + 1) * nkb / p.splits);
+      for (int kb = kb0; kb < kb1; kb += p.kps) {
+        const int nsub = kb1 - kb < p.kps ? kb1 - kb : p.kps;
+        int ok = 1;
+        if (lane == 0) {
+          if (*abort_flag || !mbar_wait(&ctl->empty[s], ph ^ 1)) {
+            record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
+            *abort_flag = 1;
+            ok = 0;
+          } else if (rank == 0) {
+            // the leader's barrier collects both CTAs' bytes; an MN-major box always brings all kps
+            // k-blocks of its chunk
+            mbar_arrive_expect_tx(&ctl->full[s], (PAIR ? 2u : 1u) * (A_KB_BYTES * (A_MN ? p.kps : nsub) +
+                                                                     p.b_kb_bytes * (B_MN ? p.kps : nsub)));
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) {
+          live = false;
+          break;
+        }
+        uint8_t* a_reg = smem + s * stage_bytes;
+        uint8_t* b_reg = a_reg + a_bytes;
+        const uint32_t fb = PAIR ? mapa_u32(smem_u32(&ctl->full[s]), 0) : 0u;
+        if (A_MN && lane < 2) {
+          uint8_t* dst = a_reg + lane * p.kps * CHUNK;
+          if (PAIR) tma_load_2d_pair(dst, &tmA, fb, m0 + 64 * lane, kb * KB);
+          else tma_load_2d(dst, &tmA, &ctl->full[s], m0 + 64 * lane, kb * KB);
+        }
+        if (B_MN && lane >= 2 && lane - 2 < bn_cta / 64) {
+          uint8_t* dst = b_reg + (lane - 2) * p.kps * CHUNK;
+          if (PAIR) tma_load_2d_pair(dst, &tmB, fb, n0 + 64 * (lane - 2), kb * KB);
+          else tma_load_2d(dst, &tmB, &ctl->full[s], n0 + 64 * (lane - 2), kb * KB);
+        }
+        const int u = (lane - 8) >> 1;
+        if (lane >= 8 && u < nsub) {
+          if (!A_MN && !(lane & 1)) {
+            uint8_t* dst = a_reg + u * A_KB_BYTES;
+            if (PAIR) tma_load_2d_pair(dst, &tmA, fb, (kb + u) * KB, m0);
+            else tma_load_2d(dst, &tmA, &ctl->full[s], (kb + u) * KB, m0);
+          }
+          if (!B_MN && (lane & 1)) {
+            uint8_t* dst = b_reg + u * p.b_kb_bytes;
+            if (PAIR) tma_load_2d_pair(dst, &tmB, fb, (kb + u) * KB, n0);
+            else tma_load_2d(dst, &tmB, &ctl->full[s], (kb + u) * KB, n0);
+          }
+        }
+        ++it;
+        if (++s == p.stages) {
+          s = 0;
+          ph ^= 1;
+        }
+        __syncwarp();
+      }
+    }
+    // none of this CTA's copies may be in flight when it exits (matters after an abort only)
+    if (lane == 0 && rank == 0)
+      for (int j = (it > p.stages ? it - p.stages : 0); j < it; ++j)
+        mbar_wait(&ctl->full[j % p.stages], (j / p.stages) & 1, 20000000ull);
+  } else if (warp == 1) {
+    // ------------------------------------------------------------- MMA issuer
+    if (lane == 0 && rank == 0) {
+      int acc_it = 0, s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      const uint32_t idesc = instr_desc_bf16(TILE_M, p.BN, A_MN, B_MN);
+      const uint32_t a_lbo = A_MN ? p.kps * CHUNK : 16, b_lbo = B_MN ? p.kps * CHUNK : 16;
+      const uint32_t a_step = A_MN ? CHUNK : A_KB_BYTES, b_step = B_MN ? CHUNK : p.b_kb_bytes;
+      const uint32_t ring = smem_u32(smem);
+      for (int w = unit; w < items && ok; w += units, ++acc_it) {
+        const int split = p.splits > 1 ? w / tiles : 0;
+        const int kb0 = static_cast<int>(static_cast<int64_t>(split) * nkb / p.splits);
+        const int kb1 = static_cast<int>(static_cast<int64_t>(split + 1) * nkb / p.splits);
+        const int buf = acc_it & 1;
+        if (*abort_flag || !mbar_wait(&ctl->acc_empty[buf], ((acc_it >> 1) & 1) ^ 1)) {
+          record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
+          *abort_flag = 1;
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t d = tmem_base + buf * ACC_COLS;
+        for (int kb = kb0; kb < kb1; kb += p.kps) {
+          const int nsub = kb1 - kb < p.kps ? kb1 - kb : p.kps;
+          if (*abort_flag || !mbar_wait(&ctl->full[s], ph)) {
+            record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
+            *abort_flag = 1;
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t a_addr = ring + s * stage_bytes, b_addr = a_addr + a_bytes;
+          for (int u = 0; u < nsub; ++u) {
+            const uint64_t ad = smem_desc_sw128(a_addr + u * a_step, a_lbo, 1024);
+            const uint64_t bd = smem_desc_sw128(b_addr + u * b_step, b_lbo, 1024);
+#pragma unroll
+            for (int k = 0; k < KB / 16; ++k) {
+              // 16 contraction elements: 32 bytes of a K-major row, 16 rows of 128 bytes MN-major
+              const uint64_t a1 = ad + static_cast<uint64_t>(k * (A_MN ? 2048 / 16 : 32 / 16));
+              const uint64_t b1 = bd + static_cast<uint64_t>(k * (B_MN ? 2048 / 16 : 32 / 16));
+              const uint32_t accum = (kb > kb0 || u > 0 || k > 0) ? 1u : 0u;
+              if (PAIR) umma_bf16_pair(d, a1, b1, idesc, accum); else umma_bf16(d, a1, b1, idesc, accum);
+            }
+          }
+          if (PAIR) umma_commit_pair(&ctl->empty[s], 3); else umma_commit(&ctl->empty[s]);
+          if (++s == p.stages) {
+            s = 0;
+            ph ^= 1;
+          }
+        }
+        if (ok) {
+          if (PAIR) umma_commit_pair(&ctl->acc_full[buf], 3); else umma_commit(&ctl->acc_full[buf]);
+        }
+      }
+      if (!ok) {      // MMAs already issued may still read the ring and write TMEM
+        if (PAIR) umma_commit_pair(&ctl->drain, 1); else umma_commit(&ctl->drain);
+        mbar_wait(&ctl->drain, 0, 20000000ull);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------- epilogue
+    const int e = warp - 2, q = warp & 3, half = e >> 2;
+    constexpr int BC = EPI == LM_DH ? 16 : 32;            // columns of a block: 64 bytes of output
+    const int nblk = p.BN / BC, jb0 = half ? (nblk + 1) >> 1 : 0, jb1 = half ? nblk : (nblk + 1) >> 1;
+    uint8_t* my = stg + e * 2 * STG_BYTES;
+    int acc_it = 0, st_it = 0;
+    const float out_scale = EPI == LM_DW ? *p.scale : 1.f;
+    for (int w = unit; w < items; w += units, ++acc_it) {
+      const int split = w / tiles;
+      int tm, tn;
+      tile_at(w - split * tiles, tiles_m, tiles_n, p.panel, tm, tn);
+      const int row0 = tm * TILE_M + rank * ROWS + q * 32, row = row0 + lane, n0 = tn * p.BN;
+      const int buf = acc_it & 1;
+      // this thread's token, fetched behind the products
+      int label = -1;
+      float nlse2 = 0.f, ratio = 0.f;
+      bool live = false;
+      if (EPI == LM_STAT) {
+        live = row < p.Mr;
+        if (live) label = p.labels[row];
+      } else if (EPI == LM_GRAD) {
+        live = row < n_live;
+        if (live) {
+          const TokenRow r = p.rows[row];
+          nlse2 = r.nlse2;
+          ratio = r.ratio;
+          label = r.label - p.v0;
+        }
+      }
+      bool got = *abort_flag ? false : mbar_wait(&ctl->acc_full[buf], (acc_it >> 1) & 1);
+      got = __all_sync(0xffffffffu, got);
+      if (!got) {
+        record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
+        *abort_flag = 1;
+        break;
+      }
+      tc_fence_after();
+      const uint32_t t_row = tmem_base + buf * ACC_COLS + (static_cast<uint32_t>(q * 32) << 16);
+      if (EPI == LM_STAT) {
+        float m = -INFINITY, sum = 0.f;
+        for (int jb = jb0; jb < jb1; ++jb) {
+          const int c0 = n0 + jb * 32;
+          if (c0 >= p.Nc) break;
+          uint32_t r[32];
+          tmem_ld_32x32(t_row + jb * 32, r);
+          tmem_wait_ld();
+          if (c0 + 32 > p.Nc) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (c0 + j >= p.Nc) r[j] = 0xff800000u;      // columns past the vocabulary: exp gives 0
+          }
+          const int at = label - c0;
+          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (at == j) p.label_logit[row] = __uint_as_float(r[j]);
+          }
+          float top = __uint_as_float(r[0]);
+#pragma unroll
+          for (int j = 1; j < 32; ++j) top = fmaxf(top, __uint_as_float(r[j]));
+          const float m1 = fmaxf(m, top), off = -m1 * LOG2E;
+          float part = 0.f;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) part += ex2(fmaf(__uint_as_float(r[j]), LOG2E, off));
+          sum = (m == -INFINITY ? 0.f : sum * ex2(fmaf(m, LOG2E, off))) + part;
+          m = m1;
+        }
+        if (live) p.part[static_cast<int64_t>(tn * 2 + half) * p.part_pitch + row] = make_float2(m, sum);
+      } else {
+        for (int jb = jb0; jb < jb1; ++jb) {
+          const int c0 = n0 + jb * BC;
+          if (c0 >= p.Nc) break;
+          uint32_t r[32];
+          if (BC == 32) tmem_ld_32x32(t_row + jb * BC, r); else tmem_ld_32x16(t_row + jb * BC, r);
+          uint8_t* ob = my + (st_it & 1) * STG_BYTES;
+          if (lane == 0) tma_store_wait_read1();      // the store that last used this buffer has read it
+          ++st_it;
+          tmem_wait_ld();
+          __syncwarp();
+          if (EPI == LM_GRAD) {
+            const int at = label - c0;
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(__uint_as_float(r[j]), LOG2E, nlse2));
+            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (at == j) v[j] -= 1.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float g[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) g[j] = live ? v[8 * i + j] * ratio : 0.f;
+              *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) =
+                  make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
+            }
+          } else if (EPI == LM_DW) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float g[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) g[j] = __uint_as_float(r[8 * i + j]) * out_scale;
+              *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) =
+                  make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+          }
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) {
+            if (EPI == LM_DH) {
+              const int y = static_cast<int>(split * p.slab_rows) + row0;
+              if (p.first) tma_store_2d(&tmOut, ob, c0, y); else tma_reduce_add_2d(&tmOut, ob, c0, y);
+            } else if (EPI == LM_GRAD || row0 < p.Mr) {
+              tma_store_2d(&tmOut, ob, c0, row0);       // clipped at the tensor's edges
+            }
+            tma_store_commit();
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR) mbar_arrive_cluster(mapa_u32(smem_u32(&ctl->acc_empty[buf]), 0));
+        else mbar_arrive(&ctl->acc_empty[buf]);
+      }
+    }
+    if (EPI != LM_STAT && lane == 0) tma_store_wait_all();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (PAIR) cluster_sync();
+  if (warp == 1) {
+    if (PAIR) tmem_dealloc_pair(tmem_base, TMEM_ALL); else tmem_dealloc(tmem_base, TMEM_ALL);
+  }
+}
+
+// lse and loss of each token from the partial maxima and sums: 32 tokens per block, 8 threads each.
+__global__ void __launch_bounds__(256) lm_combine_kernel(const float2* __restrict__ part, int parts, int64_t pitch,
+                                                         const float* __restrict__ label_logit,
+                                                         const int32_t* __restrict__ labels, int64_t T, int64_t V,
+                                                         float* __restrict__ loss, float* __restrict__ lse, int* status) {
+  __shared__ float2 s[8][33];
+  pdl_trigger();
+  pdl_wait();
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 32 + x;
+  float m = -INFINITY, sum = 0.f;
+  auto add = [&](float2 o) {
+    const float m1 = fmaxf(m, o.x);
+    if (m1 == -INFINITY && sum == 0.f && o.y == 0.f) return;      // nothing seen yet on either side
+    sum = sum * ex2((m - m1) * LOG2E) + o.y * ex2((o.x - m1) * LOG2E);
+    m = m1;
+  };
+  if (t < T)
+    for (int i = y; i < parts; i += 8) add(part[static_cast<int64_t>(i) * pitch + t]);
+  s[y][x] = make_float2(m, sum);
+  __syncthreads();
+  if (y == 0 && t < T) {
+    for (int i = 1; i < 8; ++i) add(s[i][x]);
+    const float l = m + logf(sum);
+    const int label = labels[t];
+    lse[t] = l;
+    if (label >= V) record_status(status, EFQAT_DEV_BAD_INDEX);
+    loss[t] = label >= 0 && label < V ? l - label_logit[t] : 0.f;
+  }
+}
+
+// Tokens with a target, in order: token[i] and rows[i] for i < count, slot[t] = i or -1; and max|dloss| over
+// them (1 when it is zero or not finite: the ratios are then the gradients themselves).  One block; thread k
+// owns tokens [k seg, (k + 1) seg).
+__global__ void __launch_bounds__(1024) lm_compact_kernel(const int32_t* __restrict__ labels,
+                                                          const float* __restrict__ lse,
+                                                          const float* __restrict__ dloss, int T, int64_t V,
+                                                          int* __restrict__ count, float* __restrict__ scale,
+                                                          int* __restrict__ token, int* __restrict__ slot,
+                                                          TokenRow* __restrict__ rows, int* status) {
+  __shared__ int s_cnt[32];
+  __shared__ uint32_t s_max[32];
+  pdl_trigger();
+  pdl_wait();
+  const int seg = (T + 1023) / 1024;
+  const int t0 = threadIdx.x * seg, t1 = t0 + seg < T ? t0 + seg : T;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int n = 0;
+  uint32_t top = 0;
+  for (int t = t0; t < t1; ++t) {
+    const int label = labels[t];
+    if (label >= V) record_status(status, EFQAT_DEV_BAD_INDEX);
+    if (label >= 0 && label < V) {
+      ++n;
+      top = max(top, __float_as_uint(dloss[t]) & 0x7fffffffu);
+    }
+  }
+  int incl = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 31) s_cnt[warp] = incl;
+  if (lane == 0) s_max[warp] = top;
+  __syncthreads();
+  int before = incl - n, total = 0;
+  uint32_t all = 0;
+  for (int w = 0; w < 32; ++w) {
+    if (w < warp) before += s_cnt[w];
+    total += s_cnt[w];
+    all = max(all, s_max[w]);
+  }
+  const float dmax = (all == 0 || all >= 0x7f800000u) ? 1.f : __uint_as_float(all);
+  for (int t = t0; t < t1; ++t) {
+    const int label = labels[t];
+    if (label >= 0 && label < V) {
+      TokenRow r;
+      r.nlse2 = -lse[t] * LOG2E;
+      r.ratio = __fdiv_rn(dloss[t], dmax);
+      r.label = label;
+      r.pad = 0;
+      rows[before] = r;
+      token[before] = t;
+      slot[t] = before++;
+    } else {
+      slot[t] = -1;
+    }
+  }
+  if (threadIdx.x == 0) {
+    *count = total;
+    *scale = dmax;
+  }
+}
+
+// Hidden states of the tokens with a target, gathered to the front; zeros up to the end of the last tile.
+__global__ void __launch_bounds__(256) lm_gather_kernel(const bf16* __restrict__ H, const int* __restrict__ count,
+                                                        const int* __restrict__ token, int D, bf16* __restrict__ Hc) {
+  pdl_trigger();
+  pdl_wait();
+  const int n = *count, end = ((n > 0 ? n : 1) + 255) & ~255;
+  for (int i = blockIdx.x; i < end; i += gridDim.x) {
+    const uint4* src = i < n ? reinterpret_cast<const uint4*>(H + static_cast<int64_t>(token[i]) * D) : nullptr;
+    uint4* dst = reinterpret_cast<uint4*>(Hc + static_cast<int64_t>(i) * D);
+    for (int c = threadIdx.x; c < D / 8; c += 256) dst[c] = src ? src[c] : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// dH of every token: the slabs of its row summed in order, times max|dloss|, rounded once; zero without a target.
+__global__ void __launch_bounds__(256) lm_dh_kernel(const float* __restrict__ slabs, int splits, int64_t slab_rows,
+                                                    const int* __restrict__ slot, const float* __restrict__ scale,
+                                                    int64_t T, int D, bf16* __restrict__ dH) {
+  pdl_trigger();
+  pdl_wait();
+  const float f = *scale;
+  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+    const int i = slot[t];
+    for (int c = threadIdx.x * 4; c < D; c += 1024) {
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (i >= 0)
+        for (int s = 0; s < splits; ++s) {
+          const float4 a = *reinterpret_cast<const float4*>(slabs + (s * slab_rows + i) * D + c);
+          v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+        }
+      *reinterpret_cast<uint2*>(dH + t * D + c) = make_uint2(pack2(v.x * f, v.y * f), pack2(v.z * f, v.w * f));
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host side
+struct Tiling {
+  int pair, BN;
+  int64_t tiles_m, tiles_n;
+};
+
+// Tile shape of a product [rows x cols]: the one with the fewest tile times, where a tile of BN columns
+// costs BN + 24 (its epilogue and pipeline fill) and pairs of CTAs (256 rows, half the column operand's
+// traffic) are 8 % cheaper per column.  Column steps of `unit` (64 for MN-major operands).
+Tiling choose_tiling(int64_t rows, int64_t cols, int unit, int sm_count) {
+  Tiling best = {};
+  double cost = 1e300;
+  if (rows > ROWS)
+    for (int bn = 256; bn >= 128; bn >>= 1) {
+      const int64_t tm = ceil_div(rows, 2 * ROWS), tn = ceil_div(cols, bn);
+      const double c = 0.92 * static_cast<double>(ceil_div(tm * tn, sm_count / 2)) * (bn + 24);
+      if (c < cost) {
+        cost = c;
+        best = {1, bn, tm, tn};
+      }
+    }
+  for (int bn = 256; bn >= 64; bn -= unit) {
+    const int64_t tm = ceil_div(rows, ROWS), tn = ceil_div(cols, bn);
+    const double c = static_cast<double>(ceil_div(tm * tn, sm_count)) * (bn + 24);
+    if (c < cost) {
+      cost = c;
+      best = {0, bn, tm, tn};
+    }
+  }
+  return best;
+}
+
+static const int64_t PIECE_BYTES = 256ll << 20;      // most bytes of G at a time
+
+struct BwdPlan {
+  int64_t Tp, Vc;      // padded tokens; vocabulary columns of a piece
+  int splits;
+  Tiling grad, dh, dw;
+};
+
+BwdPlan bwd_plan(int64_t T, int64_t V, int64_t D, int sm_count) {
+  BwdPlan b = {};
+  b.Tp = round_up(T, 256);
+  // pieces of equal size, whole tiles wide
+  int64_t most = PIECE_BYTES / (2 * b.Tp) / 256 * 256;
+  if (most < 256) most = 256;
+  const int64_t pieces = ceil_div(round_up(V, 256), most);
+  b.Vc = round_up(ceil_div(V, pieces), 256);
+  b.grad = choose_tiling(T, b.Vc, 32, sm_count);
+  b.dw = choose_tiling(b.Vc, D, 64, sm_count);
+  b.dh = choose_tiling(T, D, 64, sm_count);
+  // contraction split over the machine when dH has few tiles
+  const int units = b.dh.pair ? sm_count / 2 : sm_count;
+  const int64_t tiles = b.dh.tiles_m * b.dh.tiles_n, nkb = ceil_div(V < b.Vc ? V : b.Vc, KB);
+  double best = 1e300;
+  b.splits = 1;
+  for (int64_t c = 1; c <= units && c * 8 <= nkb && c * b.Tp * D * 4 <= PIECE_BYTES; ++c) {
+    const double cost = static_cast<double>(ceil_div(tiles * c, units)) / c * (1.0 + 0.01 * (c - 1));
+    if (cost < best - 1e-12) {
+      best = cost;
+      b.splits = static_cast<int>(c);
+    }
+  }
+  return b;
+}
+
+struct FwdWs {
+  float2* part; float* label_logit;
+  size_t bytes;
+};
+FwdWs carve_fwd(void* ws, int64_t T, int64_t tiles_n) {
+  FwdWs w = {};
+  char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255));
+  size_t off = 0;
+  auto take = [&](int64_t bytes) {
+    char* r = ws ? base + off : nullptr;
+    off += static_cast<size_t>(round_up(bytes, 256));
+    return r;
+  };
+  w.part = reinterpret_cast<float2*>(take(2 * tiles_n * T * 8));
+  w.label_logit = reinterpret_cast<float*>(take(T * 4));
+  w.bytes = off + 256;
+  return w;
+}
+
+struct BwdWs {
+  bf16* Hc; bf16* G; float* slabs; TokenRow* rows; int* token; int* slot; int* count; float* scale;
+  size_t bytes;
+};
+BwdWs carve_bwd(void* ws, const BwdPlan& b, int64_t T, int64_t D) {
+  BwdWs w = {};
+  char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255));
+  size_t off = 0;
+  auto take = [&](int64_t bytes) {
+    char* r = ws ? base + off : nullptr;
+    off += static_cast<size_t>(round_up(bytes, 256));
+    return r;
+  };
+  w.Hc = reinterpret_cast<bf16*>(take(b.Tp * D * 2));
+  w.G = reinterpret_cast<bf16*>(take(b.Tp * b.Vc * 2));
+  w.slabs = reinterpret_cast<float*>(take(b.splits * b.Tp * D * 4));
+  w.rows = reinterpret_cast<TokenRow*>(take(b.Tp * 16));
+  w.token = reinterpret_cast<int*>(take(T * 4));
+  w.slot = reinterpret_cast<int*>(take(T * 4));
+  w.count = reinterpret_cast<int*>(take(4));
+  w.scale = reinterpret_cast<float*>(take(4));
+  w.bytes = off + 256;
+  return w;
+}
+
+template <int A_MN, int B_MN, int EPI, int PAIR>
+bool allow() {
+  return cudaFuncSetAttribute(lm_kernel<A_MN, B_MN, EPI, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              227 * 1024) == cudaSuccess;
+}
+
+template <int A_MN, int B_MN, int EPI>
+int launch(LmParams p, const Tiling& t, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& to,
+           int sm_count, cudaStream_t st) {
+  const int bn_cta = t.pair ? t.BN / 2 : t.BN;
+  p.BN = t.BN;
+  const int units = t.pair ? sm_count / 2 : sm_count;
+  const int64_t items = t.tiles_m * t.tiles_n * p.splits;
+  const int run = static_cast<int>(items < units ? items : units);
+  const size_t smem = 1024 + static_cast<size_t>(p.stages) * p.kps * (A_KB_BYTES + bn_cta * 128) +
+                      (EPI == LM_STAT ? 0 : WORKERS * 2 * STG_BYTES) + sizeof(Ctl);
+  count_launches(1);
+  const cudaError_t e = t.pair
+      ? launch_dependent(lm_kernel<A_MN, B_MN, EPI, 1>, 2u * run, THREADS, smem, st, 2, ta, tb, to, p)
+      : launch_dependent(lm_kernel<A_MN, B_MN, EPI, 0>, run, THREADS, smem, st, 1, ta, tb, to, p);
+  return e == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
+}
+
+// Ring of the launch: stages of two k-blocks when three of them fit, else of one.
+void set_ring(LmParams* p, const Tiling& t, bool staging) {
+  const int bn_cta = t.pair ? t.BN / 2 : t.BN;
+  p->b_kb_bytes = bn_cta * 128;
+  const int sub = A_KB_BYTES + p->b_kb_bytes;
+  const int budget = 227 * 1024 - 1024 - static_cast<int>(sizeof(Ctl)) - (staging ? WORKERS * 2 * STG_BYTES : 0);
+  p->kps = budget / (2 * sub) >= 3 ? 2 : 1;
+  p->stages = budget / (p->kps * sub);
+  if (p->stages > MAX_RING) p->stages = MAX_RING;
+}
+
+// Tile columns per panel: as many as keep their slice of the column operand within 32 MB of L2.
+int panel_of(const Tiling& t, int64_t contraction) {
+  int64_t n = (32ll << 20) / (static_cast<int64_t>(t.BN) * contraction * 2);
+  if (n < 1) n = 1;
+  return static_cast<int>(n < t.tiles_n ? n : t.tiles_n);
+}
+
+}  // namespace
+
+int lm_loss_init() {
+  const bool ok = allow<0, 0, LM_STAT, 0>() && allow<0, 0, LM_STAT, 1>() && allow<0, 0, LM_GRAD, 0>() &&
+                  allow<0, 0, LM_GRAD, 1>() && allow<0, 1, LM_DH, 0>() && allow<0, 1, LM_DH, 1>() &&
+                  allow<1, 1, LM_DW, 0>() && allow<1, 1, LM_DW, 1>();
+  return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
+}
+
+void lm_loss_workspace_bytes(int64_t T, int64_t V, int64_t D, int sm_count, size_t* fwd, size_t* bwd) {
+  *fwd = carve_fwd(nullptr, T, choose_tiling(T, V, 32, sm_count).tiles_n).bytes;
+  *bwd = carve_bwd(nullptr, bwd_plan(T, V, D, sm_count), T, D).bytes;
+}
+
+int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t T, int64_t V, int64_t D, float* loss,
+                    float* lse, void* ws, int* status, int sm_count, cudaStream_t st) {
+  const Tiling t = choose_tiling(T, V, 32, sm_count);
+  const FwdWs w = carve_fwd(ws, T, t.tiles_n);
+  CUtensorMap ta, tb;
+  int rc = tensor_map_2d(&ta, H, 1, T, D, D, ROWS, 128);
+  if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, W, 1, V, D, D, t.pair ? t.BN / 2 : t.BN, 128);
+  if (rc != EFQAT_OK) return rc;
+  LmParams p = {};
+  p.Mr = T; p.Nc = V;
+  p.nkb = static_cast<int>(ceil_div(D, KB));
+  p.splits = 1;
+  p.panel = panel_of(t, D);
+  p.labels = labels;
+  p.part = w.part; p.label_logit = w.label_logit; p.part_pitch = T;
+  p.status = status;
+  set_ring(&p, t, false);
+  rc = launch<0, 0, LM_STAT>(p, t, ta, tb, ta, sm_count, st);
+  if (rc != EFQAT_OK) return rc;
+  count_launches(1);
+  return launch_dependent(lm_combine_kernel, static_cast<unsigned>(ceil_div(T, 32)), 256, 0, st, 1,
+                          static_cast<const float2*>(w.part), static_cast<int>(2 * t.tiles_n), T,
+                          static_cast<const float*>(w.label_logit), labels, T, V, loss, lse, status) == cudaSuccess
+             ? EFQAT_OK : EFQAT_ERR_CUDA;
+}
+
+int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const float* lse, const float* dloss,
+                    int64_t T, int64_t V, int64_t D, bf16* dH, bf16* dW, void* ws, int* status, int sm_count,
+                    cudaStream_t st) {
+  const BwdPlan b = bwd_plan(T, V, D, sm_count);
+  const BwdWs w = carve_bwd(ws, b, T, D);
+  bool ok = true;
+  count_launches(2);
+  ok = ok && launch_dependent(lm_compact_kernel, 1u, 1024u, 0, st, 1, labels, lse, dloss, static_cast<int>(T), V,
+                              w.count, w.scale, w.token, w.slot, w.rows, status) == cudaSuccess;
+  const unsigned gather = static_cast<unsigned>(b.Tp < sm_count * 8 ? b.Tp : sm_count * 8);
+  ok = ok && launch_dependent(lm_gather_kernel, gather, 256u, 0, st, 1, H, static_cast<const int*>(w.count),
+                              static_cast<const int*>(w.token), static_cast<int>(D), w.Hc) == cudaSuccess;
+  if (!ok) return EFQAT_ERR_CUDA;
+  for (int64_t v0 = 0; v0 < V; v0 += b.Vc) {
+    const int64_t nv = V - v0 < b.Vc ? V - v0 : b.Vc;
+    const bf16* Wc = W + v0 * D;
+    CUtensorMap ta, tb, to;
+    // G = softmax gradient of this piece
+    Tiling t = b.grad;
+    t.tiles_n = ceil_div(nv, t.BN);
+    int rc = tensor_map_2d(&ta, w.Hc, 1, b.Tp, D, D, ROWS, 128);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, t.pair ? t.BN / 2 : t.BN, 128);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, w.G, 1, b.Tp, nv, b.Vc, 32, 64);
+    if (rc != EFQAT_OK) return rc;
+    LmParams p = {};
+    p.Mr = T; p.Nc = nv;
+    p.n_rows = w.count;
+    p.nkb = static_cast<int>(ceil_div(D, KB));
+    p.splits = 1;
+    p.panel = panel_of(t, D);
+    p.rows = w.rows; p.v0 = static_cast<int>(v0);
+    p.status = status;
+    set_ring(&p, t, true);
+    rc = launch<0, 0, LM_GRAD>(p, t, ta, tb, to, sm_count, st);
+    if (rc != EFQAT_OK) return rc;
+    // dH += G Wc
+    t = b.dh;
+    rc = tensor_map_2d(&ta, w.G, 1, b.Tp, nv, b.Vc, ROWS, 128);
+    p = LmParams{};
+    p.Mr = T; p.Nc = D;
+    p.n_rows = w.count;
+    p.nkb = static_cast<int>(ceil_div(nv, KB));
+    p.splits = b.splits < p.nkb ? b.splits : p.nkb;
+    p.panel = static_cast<int>(t.tiles_n);
+    p.first = v0 == 0; p.slab_rows = b.Tp;
+    p.status = status;
+    set_ring(&p, t, true);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, KB * p.kps, 128);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, w.slabs, 0, b.splits * b.Tp, D, D, 32, 64);
+    if (rc == EFQAT_OK) rc = launch<0, 1, LM_DH>(p, t, ta, tb, to, sm_count, st);
+    if (rc != EFQAT_OK) return rc;
+    // dW of this piece = G^T H
+    t = b.dw;
+    t.tiles_m = ceil_div(nv, t.pair ? 2 * ROWS : ROWS);
+    p = LmParams{};
+    p.Mr = nv; p.Nc = D;
+    p.n_rows = w.count;
+    p.splits = 1;
+    p.panel = static_cast<int>(t.tiles_n);
+    p.scale = w.scale;
+    p.status = status;
+    set_ring(&p, t, true);
+    rc = tensor_map_2d(&ta, w.G, 1, b.Tp, nv, b.Vc, KB * p.kps, 128);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, w.Hc, 1, b.Tp, D, D, KB * p.kps, 128);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, dW + v0 * D, 1, nv, D, D, 32, 64);
+    if (rc == EFQAT_OK) rc = launch<1, 1, LM_DW>(p, t, ta, tb, to, sm_count, st);
+    if (rc != EFQAT_OK) return rc;
+  }
+  const unsigned grid = static_cast<unsigned>(T < sm_count * 8 ? T : sm_count * 8);
+  count_launches(1);
+  return launch_dependent(lm_dh_kernel, grid, 256u, 0, st, 1, static_cast<const float*>(w.slabs), b.splits, b.Tp,
+                          static_cast<const int*>(w.slot), static_cast<const float*>(w.scale), T, static_cast<int>(D),
+                          dH) == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
+}
+
+}  // namespace efqat

@@ -173,3 +173,16 @@ def test_row_operator_queries(lib):
         assert e.value.code == code
     assert lib.efqat_gelu_fwd(None, 1, None, 4, 16, None, None, None) == -1
     assert lib.efqat_layer_norm_fwd(None, 1, None, 4, 16, None, None, 1e-5, None, None, None, None, None) == -1
+
+
+def test_lm_loss_queries(lib):
+    """Workspace of the language-model loss: far below the logits, empty without tokens, and the refusals."""
+    fwd, bwd = B.lm_loss_workspace_bytes(8192, 128000, 2048)
+    assert fwd < 8192 * 128000 * 4 // 32 and bwd < 8192 * 128000 * 2 // 4
+    assert B.lm_loss_workspace_bytes(0, 100, 64) == (0, 0)
+    for args, code in (((4, 0, 64), -2), ((-1, 10, 64), -2), ((4, 10, 60), -3), ((4, 1 << 25, 64), -11)):
+        with pytest.raises(B.EfqatError) as e:
+            B.lm_loss_workspace_bytes(*args)
+        assert e.value.code == code
+    assert lib.efqat_lm_loss_fwd(None, None, None, None, 1, 1, 8, None, None, None, 0, None) == -1
+    assert lib.efqat_lm_loss_bwd(None, None, None, None, None, None, 1, 1, 8, None, None, None, 0, None) == -1
