@@ -347,6 +347,7 @@ int efqat_create(efqat_ctx** out, int device) {
       cudaMalloc(&c->d_status, 256) != cudaSuccess || cudaMemset(c->d_status, 0, 256) != cudaSuccess)
     rc = EFQAT_ERR_CUDA;
   if (rc == EFQAT_OK) rc = gemm_init();
+  if (rc == EFQAT_OK) rc = norm_init();
   if (rc == EFQAT_OK) rc = lm_loss_init();
   cudaSetDevice(prev);
   if (rc != EFQAT_OK) {
@@ -1144,8 +1145,9 @@ int efqat_layer_norm_fwd(efqat_ctx* ctx, int dtype, const void* x, int64_t M, in
   if (rc == EFQAT_OK && M > 0 && (!mean || !rstd)) rc = EFQAT_ERR_NULL;
   if (rc != EFQAT_OK || M == 0) return rc;
   Entered in(ctx);
-  launch_norm_fwd(dtype, x, nullptr, M, C, gamma, beta_or_null, eps, y, mean, rstd, save_or_null, ctx->sm_count, stream);
-  return last_error();
+  rc = launch_norm_fwd(dtype, x, nullptr, M, C, gamma, beta_or_null, eps, y, mean, rstd, save_or_null, ctx->d_status,
+                       ctx->sm_count, stream);
+  return rc != EFQAT_OK ? rc : last_error();
 }
 
 int efqat_layer_norm_bwd(efqat_ctx* ctx, int dtype, const void* dY, const void* x_or_null,
@@ -1169,9 +1171,9 @@ int efqat_layer_norm_bwd(efqat_ctx* ctx, int dtype, const void* dY, const void* 
   if (!ws || ws_bytes < layer_norm_workspace_bytes(M, C, ctx->sm_count) + 256) return EFQAT_ERR_WORKSPACE;
   Entered in(ctx);
   float* part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255));
-  launch_norm_bwd(dtype, dY, x_or_null, saved_or_null, M, C, gamma, mean, rstd, dX, dgamma, dbeta, part, ctx->sm_count,
-                  stream);
-  return last_error();
+  rc = launch_norm_bwd(dtype, dY, x_or_null, saved_or_null, M, C, gamma, mean, rstd, dX, dgamma, dbeta, part,
+                       ctx->d_status, ctx->sm_count, stream);
+  return rc != EFQAT_OK ? rc : last_error();
 }
 
 int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* saved, int64_t M, int64_t C,
@@ -1185,9 +1187,9 @@ int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* save
   if (rc == EFQAT_OK && M > 0 && (!mean || !rstd)) rc = EFQAT_ERR_NULL;
   if (rc != EFQAT_OK || M == 0) return rc;
   Entered in(ctx);
-  launch_norm_fwd(dtype, nullptr, saved, M, C, gamma, beta_or_null, 0.f, y, const_cast<float*>(mean),
-                  const_cast<float*>(rstd), nullptr, ctx->sm_count, stream);
-  return last_error();
+  rc = launch_norm_fwd(dtype, nullptr, saved, M, C, gamma, beta_or_null, 0.f, y, const_cast<float*>(mean),
+                       const_cast<float*>(rstd), nullptr, ctx->d_status, ctx->sm_count, stream);
+  return rc != EFQAT_OK ? rc : last_error();
 }
 
 // ---- language-model loss --------------------------------------------------------------------

@@ -4,11 +4,11 @@
 //   gelu fwd   x -> y [, (codes, scales)]       recompute  (codes, scales) -> gelu(x~)
 //   gelu bwd   dY, x or (codes, scales) -> dX
 //
-// GELU: Phi(x) = 1 - P(t) e / 2 for x >= 0 and P(t) e / 2 below, with e = exp(-x^2 / 2),
-// t = 1 / (1 + p |x| / sqrt 2) and the degree-5 polynomial P of Abramowitz & Stegun, Handbook of
-// Mathematical Functions, 7.1.26 (absolute error of erf at most 1.5e-7).  The slope
-// Phi(x) + x e / sqrt(2 pi) needs the same exponential, so either direction costs two
-// special-function operations per element (a reciprocal and a power of two).
+// GELU: 1 - Phi(|x|) = P(t) t e / 2 with e = exp(-x^2 / 2), t = 1 / (1 + p |x| / sqrt 2) and the
+// degree-4 polynomial P of Abramowitz & Stegun, Handbook of Mathematical Functions, 7.1.26 (absolute
+// error of erf at most 1.5e-7).  The slope Phi(x) + x e / sqrt(2 pi) needs the same exponential, so
+// either direction costs two special-function operations per element (a reciprocal and a power of
+// two); the rest goes through the packed fp32 instructions, two elements to an issue slot.
 #include "rowops.cuh"
 
 namespace efqat {
@@ -27,20 +27,32 @@ __device__ __forceinline__ float ex2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// For two values: Phi(|x|) - 1/2 = 1/2 - P(t) t e / 2, and e = exp(-x^2 / 2) on the side.
+__device__ __forceinline__ pair_t normal_half(pair_t x, pair_t& e) {
+  const float c = 0.3275911f * 0.70710678118654752f;
+  const float2 v = halves(x), z = halves(mul2(mul2(x, both(-0.5f * 1.4426950408889634f)), x));
+  const pair_t t = pair_of(rcp_approx(fmaf(fabsf(v.x), c, 1.f)), rcp_approx(fmaf(fabsf(v.y), c, 1.f)));
+  e = pair_of(ex2_approx(z.x), ex2_approx(z.y));
+  pair_t p = fma2(both(-0.5f * 1.061405429f), t, both(0.5f * 1.453152027f));
+  p = fma2(p, t, both(-0.5f * 1.421413741f));
+  p = fma2(p, t, both(0.5f * 0.284496736f));
+  p = fma2(p, t, both(-0.5f * 0.254829592f));
+  return fma2(mul2(p, t), e, both(0.5f));
+}
+__device__ __forceinline__ pair_t with_signs(pair_t v, pair_t of) { return v | (of & 0x8000000080000000ull); }
 
-// Phi(x), and e = exp(-x^2 / 2) on the side.
-__device__ __forceinline__ float normal_cdf(float x, float& e) {
-  const float ax = fabsf(x);
-  const float t = rcp_approx(fmaf(ax, 0.3275911f * 0.70710678118654752f, 1.f));
-  e = ex2_approx(x * x * (-0.5f * 1.4426950408889634f));
-  // half the polynomial's coefficients: Phi takes half of erfc
-  float p = 0.5f * 1.061405429f;
-  p = fmaf(p, t, 0.5f * -1.453152027f);
-  p = fmaf(p, t, 0.5f * 1.421413741f);
-  p = fmaf(p, t, 0.5f * -0.284496736f);
-  p = fmaf(p, t, 0.5f * 0.254829592f);
-  const float tail = p * t * e;
-  return x < 0.f ? tail : 1.f - tail;
+// x Phi(x) with Phi(x) = 1/2 + sign(x) (Phi(|x|) - 1/2)
+__device__ __forceinline__ pair_t gelu2(pair_t x) {
+  pair_t e;
+  const pair_t h = normal_half(x, e);
+  return mul2(x, add2(with_signs(h, x), both(0.5f)));
+}
+
+// Phi(x) + x phi(x)
+__device__ __forceinline__ pair_t gelu_slope2(pair_t x) {
+  pair_t e;
+  const pair_t h = normal_half(x, e);
+  return add2(fma2(mul2(x, both(0.3989422804014327f)), e, both(0.5f)), with_signs(h, x));
 }
 
 struct RowArgs {
@@ -98,7 +110,7 @@ __global__ void __launch_bounds__(256) ckpt_kernel(RowArgs a) {
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
       const uint32_t g = g0 + (half & 1u) + u * halves;
-      float v[8];
+      pair_t v[4];
       if (SRC == 0) xv[u].get(v); else ckpt_values(cv[u], sc[u], v);
       if (SAVE) {
         const GroupScale gs = ckpt_group_scale(v);
@@ -108,25 +120,18 @@ __global__ void __launch_bounds__(256) ckpt_kernel(RowArgs a) {
         }
       }
       if (SAVE && ACT == ACT_NONE) continue;
-      float o[8];
+      pair_t o[4];
       if (ACT == ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = v[i];
+        for (int i = 0; i < 4; ++i) o[i] = v[i];
       } else if (ACT == ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float e;
-          o[i] = v[i] * normal_cdf(v[i], e);
-        }
+        for (int i = 0; i < 4; ++i) o[i] = gelu2(v[i]);
       } else {
-        float d[8];
+        pair_t d[4];
         dv[u].get(d);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float e;
-          const float phi = normal_cdf(v[i], e);
-          o[i] = d[i] * fmaf(v[i] * 0.3989422804014327f, e, phi);
-        }
+        for (int i = 0; i < 4; ++i) o[i] = mul2(d[i], gelu_slope2(v[i]));
       }
       if (ok[u]) store8(static_cast<T*>(a.y) + at[u], o);
     }

@@ -112,13 +112,14 @@ void launch_ckpt(int dtype, int act, const void* x, const efqat_ckpt* in, const 
 
 // ---- norm.cu ------------------------------------------------------------------------
 // in given: y from the checkpoint and the given mean / rstd; else mean and rstd are written.
-void launch_norm_fwd(int dtype, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
-                     const float* beta, float eps, void* y, float* mean, float* rstd, const efqat_ckpt* out,
-                     int sm_count, cudaStream_t st);
+int norm_init();      // per device, with that device current (efqat_create)
+int launch_norm_fwd(int dtype, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
+                    const float* beta, float eps, void* y, float* mean, float* rstd, const efqat_ckpt* out,
+                    int* status, int sm_count, cudaStream_t st);
 // part: layer_norm_workspace_bytes() of partial sums.
-void launch_norm_bwd(int dtype, const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C,
-                     const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta,
-                     float* part, int sm_count, cudaStream_t st);
+int launch_norm_bwd(int dtype, const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C,
+                    const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta,
+                    float* part, int* status, int sm_count, cudaStream_t st);
 size_t layer_norm_workspace_bytes(int64_t M, int64_t C, int sm_count);
 
 // ---- lmloss.cu ----------------------------------------------------------------------

@@ -5,17 +5,32 @@
 //   g  = dY gamma,  xh = (x - mean) rstd,  dX = rstd (g - mean_c(g) - xh mean_c(g xh))
 //   dgamma = sum_m dY xh,  dbeta = sum_m dY
 //
-// A row belongs to a team of `team` warps, each lane holding NV vectors of 8 columns in registers,
-// so every tensor is read and written once.  Rows of up to a warp's reach need shuffles only;
-// wider ones exchange one partial sum per warp through shared memory.  The variance is formed from
-// the centred values (no cancellation for rows far from zero).
+// HBM-bound: every tensor is touched once.  Persistent blocks, one per SM, whose warps form teams of
+// 1, 2, 4, 8 or 16: a team takes a row, a lane up to 32 of its columns (8, 16 or 32 lanes and one
+// warp where rows are short), the same columns in every row, so that the running dgamma and dbeta
+// stay in registers.  Each team keeps a ring of its next rows in shared memory, filled by bulk copies
+// that it requests itself as soon as it has read a row; teams of one warp (up to 1024 columns) never
+// wait for each other.
+//
+// A warp forms the variance around the mean of its own columns, and the warps' parts are joined
+// exactly (M2 = sum M2_w + sum n_w (mean_w - mean)^2): no cancellation for rows far from zero, one
+// exchange between the warps of a team per row.  Pairs of columns go through the packed fp32
+// instructions, which halves the issue slots of the element work.
 #include "rowops.cuh"
 
 namespace efqat {
 
+using namespace ptx;
+
 namespace {
 
-static const int NORM_THREADS = 512;    // most threads of a block
+static const int RING_MAX = 8;
+static const int WHOLE_BLOCK = 15;            // barrier id; teams of several warps use 1 + team (at most 8)
+static const int ITEM_BYTES = 2048;           // short rows: as many to a copy as make up about this
+// Warps of a block and bytes of its ring: the forward hides its row's chain of reductions behind other
+// rows, the backward wants the registers of few warps (it holds a row's x and dY and its 64 sums).
+static const int FWD_WARPS = 16, BWD_WARPS = 8, WIDE_WARPS = 16;
+static const int FWD_RING = 64 * 1024, BWD_RING = 160 * 1024;
 
 struct NormArgs {
   const void* x; const int8_t* codes_in; const float* scales_in;
@@ -25,217 +40,404 @@ struct NormArgs {
   float* part;                                            // backward: [gridDim.x][2][C] partial dgamma, dbeta
   int64_t M;
   int C, G, team;                                         // columns, checkpoint groups per row, warps per row
+  int R, stages, stage_bytes, items;                      // rows per item (copy), stages per team
+  int* status;
 };
 
-// Sum of two values over a team.  Teams of one warp: shuffles.  Larger teams are whole blocks.
-// `slot` alternates so that one barrier per exchange is enough.
-__device__ __forceinline__ float2 team_sum(float2 v, int team, float2* s_red, int& slot) {
-  v.x = warp_sum(v.x);
-  v.y = warp_sum(v.y);
-  if (team == 1) return v;
-  float2* red = s_red + slot * 32;
-  slot ^= 1;
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  float2 t = make_float2(0.f, 0.f);
-  for (int w = 0; w < team; ++w) {
-    const float2 o = red[w];
-    t.x += o.x;
-    t.y += o.y;
-  }
-  return t;
+struct __align__(16) NormCtl {
+  uint64_t full[16 * RING_MAX];         // [team][stage]
+  float4 red[2][16];                    // one entry per warp, two sets in turn
+  int abort_flag;
+};
+
+// Bytes of an item of R rows in the ring: x (or its codes), then (backward) dY.
+template <typename T, int SRC, int BWD>
+__host__ __device__ __forceinline__ int item_bytes(int R, int C) {
+  return (R * C * ((SRC ? 1 : static_cast<int>(sizeof(T))) + (BWD ? static_cast<int>(sizeof(T)) : 0)) + 127) & ~127;
 }
 
-template <typename T, int NV, int SRC, int SAVE>
-__global__ void __launch_bounds__(NORM_THREADS) norm_fwd_kernel(NormArgs a) {
-  __shared__ float2 s_red[64];
-  pdl_trigger();
-  pdl_wait();
-  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int teams = warps / a.team;                     // 1 when a team has several warps
-  const int tl = a.team == 1 ? lane : threadIdx.x;      // lane within the team
-  const int stride = a.team * 32 * 8;
-  int slot = 0;
-  const float inv_c = 1.f / static_cast<float>(a.C);
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * teams + (a.team == 1 ? warp : 0); row < a.M;
-       row += static_cast<int64_t>(gridDim.x) * teams) {
-    float v[NV][8];
-    const int64_t base = row * a.C;
+// Waits unless something has already run out; a wait that runs out is reported and the block goes on
+// (on whatever the ring holds), so that no warp is left alone at a barrier of its team.
+__device__ __forceinline__ void norm_wait(uint64_t* bar, uint32_t parity, NormCtl* ctl, int* status) {
+  if (mbar_try_wait(bar, parity)) return;
+  volatile int* flag = &ctl->abort_flag;
+  if (*flag) return;
+  if (!mbar_wait(bar, parity)) {
+    record_status(status, EFQAT_DEV_WAIT_TIMEOUT);
+    *flag = 1;
+  }
+}
+
+// One thread: requests an item into a stage of its team's ring (nothing past the last item, or after a
+// wait ran out).  The team has read what the stage held; the proxy fence orders those reads before
+// the copy's writes.
+template <typename T, int SRC, int BWD>
+__device__ __forceinline__ void norm_fetch(const NormArgs& a, int64_t item, uint8_t* st, uint64_t* bar, NormCtl* ctl,
+                                           int& requested) {
+  if (item >= a.items || *static_cast<volatile int*>(&ctl->abort_flag)) return;
+  ++requested;
+  const int64_t row0 = item * a.R;
+  const int rows = a.M - row0 < a.R ? static_cast<int>(a.M - row0) : a.R;
+  const uint32_t n = static_cast<uint32_t>(rows) * a.C;
+  const uint32_t xb = n * (SRC ? 1u : static_cast<uint32_t>(sizeof(T))), db = BWD ? n * static_cast<uint32_t>(sizeof(T)) : 0u;
+  fence_proxy_async();
+  mbar_arrive_expect_tx(bar, xb + db);
+  if (SRC) bulk_load(st, a.codes_in + row0 * a.C, xb, bar);
+  else bulk_load(st, static_cast<const T*>(a.x) + row0 * a.C, xb, bar);
+  if (BWD) bulk_load(st + a.R * a.C * (SRC ? 1 : static_cast<int>(sizeof(T))), static_cast<const T*>(a.dy) + row0 * a.C, db, bar);
+}
+
+// After a wait ran out: none of the team's copies may be in flight when the block exits.
+__device__ __forceinline__ void norm_drain(uint64_t* full, int stages, int requested, NormCtl* ctl) {
+  if (!*static_cast<volatile int*>(&ctl->abort_flag)) return;
+  for (int j = requested > stages ? requested - stages : 0; j < requested; ++j)
+    mbar_wait(&full[j % stages], (j / stages) & 1, 20000000ull);
+}
+
+__device__ __forceinline__ NormCtl* norm_setup(const NormArgs& a, int teams, uint8_t* at) {
+  NormCtl* ctl = reinterpret_cast<NormCtl*>(at);
+  if (threadIdx.x < teams * a.stages) mbar_init(&ctl->full[threadIdx.x], 1);
+  if (threadIdx.x == 0) ctl->abort_flag = 0;
+  fence_barrier_init();
+  __syncthreads();
+  return ctl;
+}
+
+// 8 columns of a row in shared memory, by type and source (SRC 1: codes of the given scale).
+template <typename T, int SRC>
+__device__ __forceinline__ void row_load(uint32_t addr, float scale, pair_t (&v)[4]) {
+  if (SRC) ckpt_values(lds64(addr), scale, v);
+  else if (sizeof(T) == 2) unpack8(lds128(addr), v);
+  else unpack8(lds128(addr), lds128(addr + 16), v);
+}
+
+// A parameter vector in shared memory as two planes of C / 2 floats: the first and the second four of
+// every 8 columns, so that neighbouring lanes read neighbouring 16 bytes.
+__device__ __forceinline__ void planes_fill(float* s, const float* g, int C) {
+  float4* d = reinterpret_cast<float4*>(s);
+  for (int i = threadIdx.x; i < C / 4; i += blockDim.x)
+    d[(i & 1) * (C / 8) + (i >> 1)] = g ? reinterpret_cast<const float4*>(g)[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+}
+__device__ __forceinline__ void planes_load(uint32_t addr, uint32_t plane, pair_t (&v)[4]) {
+  unpack8(lds128(addr), lds128(addr + plane), v);
+}
+
+// Sum over the LANES lanes of a row.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = tl * 8 + j * stride;
-      if (SRC == 0) {
-        Vec8<T> r;
-        r.zero();
-        if (c < a.C) r.load(static_cast<const T*>(a.x) + base + c);
-        r.get(v[j]);
-      } else {
-        uint2 w = make_uint2(0u, 0u);
-        float s = 0.f;
-        if (c < a.C) {
-          w = *reinterpret_cast<const uint2*>(a.codes_in + base + c);
-          s = a.scales_in[row * a.G + c / CKPT_GROUP];
-        }
-        ckpt_values(w, s, v[j]);
-      }
-    }
-    float mean, rstd;
-    if (SRC == 0) {
-      float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s.x += v[j][i];
-      mean = team_sum(s, a.team, s_red, slot).x * inv_c;
-      s = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        if (tl * 8 + j * stride < a.C) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float d = v[j][i] - mean;
-            s.x = fmaf(d, d, s.x);
-          }
-        }
-      }
-      const float var = team_sum(s, a.team, s_red, slot).x * inv_c;
-      rstd = 1.f / sqrtf(var + a.eps);
-      if (tl == 0) {
-        a.mean[row] = mean;
-        a.rstd[row] = rstd;
-      }
-    } else {
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float pair_sum(pair_t v) {
+  const float2 f = halves(v);
+  return f.x + f.y;
+}
+
+// Where a lane stands: WARPS warps in teams of a.team, LANES lanes to a row (32 unless rows are short).
+template <int WARPS, int LANES>
+struct Place {
+  int lane, team, teams, tw, sub, c0, stride;
+  __device__ __forceinline__ explicit Place(const NormArgs& a) {
+    const int w = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    team = w / a.team;
+    teams = WARPS / a.team;
+    tw = w - team * a.team;
+    sub = lane / LANES;
+    c0 = (tw * 32 + (lane & (LANES - 1))) * 8;
+    stride = a.team * 256;
+  }
+};
+
+// Statistics of a lane's row and the scales of its checkpoint groups: asked for one row ahead, so that
+// their latency lies behind a row's work.
+template <int NV, int SRC>
+struct RowStats {
+  float mean, rstd, scale[NV];
+  __device__ __forceinline__ void ask(const NormArgs& a, int64_t row, int c0, int stride) {
+    if (row < a.M) {
       mean = a.mean[row];
       rstd = a.rstd[row];
-    }
+      if (SRC) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = tl * 8 + j * stride;
-      if (SAVE) {
-        const GroupScale gs = ckpt_group_scale(v[j]);
-        if (c < a.C) {
-          *reinterpret_cast<uint2*>(a.codes_out + base + c) = ckpt_codes(v[j], gs);
-          if ((tl & 15) == 0) a.scales_out[row * a.G + c / CKPT_GROUP] = gs.scale;
+        for (int j = 0; j < NV; ++j) {
+          const int c = c0 + j * stride;
+          scale[j] = c < a.C ? a.scales_in[row * a.G + c / CKPT_GROUP] : 0.f;
         }
-      }
-      if (c < a.C) {
-        float o[8], gm[8], bt[8];
-        Vec8<float> p;
-        p.load(a.gamma + c);
-        p.get(gm);
-        if (a.beta) p.load(a.beta + c); else p.zero();
-        p.get(bt);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = fmaf((v[j][i] - mean) * rstd, gm[i], bt[i]);
-        store8(static_cast<T*>(a.y) + base + c, o);
       }
     }
   }
-}
+};
 
-// Backward.  A block keeps the running dgamma / dbeta of its rows in registers (each lane owns the
-// same columns in every row) and writes one partial row of each at the end.
-template <typename T, int NV, int SRC>
-__global__ void __launch_bounds__(NORM_THREADS) norm_bwd_kernel(NormArgs a) {
-  __shared__ float2 s_red[64];
-  extern __shared__ float s_part[];      // teams > 1: [teams][2][C]
+// KIND 0: y, mean, rstd; 1: and the checkpoint of x; 2: y from a checkpoint and the given statistics.
+// FULL: every lane's NV vectors lie within the row (C = 256 NV team).
+template <typename T, int NV, int KIND, int FULL, int LANES>
+__global__ void __launch_bounds__(32 * FWD_WARPS, 1) norm_fwd_kernel(NormArgs a) {
+  constexpr int SRC = KIND == 2, ES = SRC ? 1 : static_cast<int>(sizeof(T)), AT_ONCE = 32 / LANES;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const Place<FWD_WARPS, LANES> me(a);
+  float* s_gamma = reinterpret_cast<float*>(smem + me.teams * a.stages * a.stage_bytes);
+  NormCtl* ctl = norm_setup(a, me.teams, reinterpret_cast<uint8_t*>(s_gamma + 2 * a.C));
+  uint8_t* ring = smem + me.team * a.stages * a.stage_bytes;
+  uint64_t* full = ctl->full + me.team * a.stages;
+  const int first = blockIdx.x * me.teams + me.team, step = gridDim.x * me.teams;
+  const bool leader = me.tw == 0 && me.lane == 0;
+  int requested = 0;
   pdl_trigger();
   pdl_wait();
-  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int teams = warps / a.team;
-  const int tl = a.team == 1 ? lane : threadIdx.x;
-  const int stride = a.team * 32 * 8;
-  int slot = 0;
-  const float inv_c = 1.f / static_cast<float>(a.C);
-  float dg[NV][8], db[NV][8];
+  if (leader)
+    for (int s = 0; s < a.stages; ++s)
+      norm_fetch<T, SRC, 0>(a, static_cast<int64_t>(first) + s * step, ring + s * a.stage_bytes, &full[s], ctl, requested);
+  planes_fill(s_gamma, a.gamma, a.C);
+  planes_fill(s_gamma + a.C, a.beta, a.C);
+  __syncthreads();
+  const uint32_t gamma_at = smem_u32(s_gamma) + me.c0 * 2, beta_at = gamma_at + a.C * 4, plane = a.C * 2;
+  int mine = 0;                       // this warp's columns
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int left = a.C - (me.tw * 256 + j * me.stride);
+    mine += left < 0 ? 0 : (left < 256 ? left : 256);
+  }
+  const float inv_c = 1.f / static_cast<float>(a.C), inv_mine = mine ? 1.f / static_cast<float>(mine) : 0.f;
+  int slot = 0, s = 0;
+  uint32_t ph = 0;
+  RowStats<NV, SRC> next = {}, now;
+  if (SRC) next.ask(a, static_cast<int64_t>(first) * a.R + me.sub, me.c0, me.stride);
+  for (int64_t item = first; item < a.items; item += step) {
+    const int64_t row0 = item * a.R;
+    const int rows = a.M - row0 < a.R ? static_cast<int>(a.M - row0) : a.R;
+    uint8_t* st = ring + s * a.stage_bytes;
+    norm_wait(&full[s], ph, ctl, a.status);
+    for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
+      const int r = r0 + me.sub;
+      const bool live = AT_ONCE == 1 || r < rows;
+      const int64_t row = row0 + r;
+      if (SRC) {
+        now = next;
+        next.ask(a, (r0 + AT_ONCE < rows ? row + AT_ONCE : (item + step) * a.R + me.sub), me.c0, me.stride);
+      }
+      const uint32_t x_at = smem_u32(st) + (r * a.C + me.c0) * ES;
+      pair_t v[NV][4];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = me.c0 + j * me.stride;
+        if (FULL || (c < a.C && live)) {
+          row_load<T, SRC>(x_at + j * me.stride * ES, SRC ? now.scale[j] : 0.f, v[j]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[j][i] = 0;
+        }
+      }
+      float mean, rstd;
+      if (SRC == 0) {
+        pair_t t[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t[i & 1] = add2(t[i & 1], v[j][i]);
+        mean = lanes_sum<LANES>(pair_sum(add2(t[0], t[1]))) * inv_mine;
+        t[0] = t[1] = 0;
+        const pair_t off = both(-mean);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          if (FULL || me.c0 + j * me.stride < a.C) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const pair_t d = add2(v[j][i], off);
+              t[i & 1] = fma2(d, d, t[i & 1]);
+            }
+          }
+        }
+        float m2 = lanes_sum<LANES>(pair_sum(add2(t[0], t[1])));
+        if (a.team > 1) {
+          float4* red = ctl->red[slot] + me.team * a.team;
+          slot ^= 1;
+          if (me.lane == 0) red[me.tw] = make_float4(mean, m2, static_cast<float>(mine), 0.f);
+          named_barrier(1 + me.team, a.team * 32);
+          const float4 o = red[me.lane & (a.team - 1)];
+          mean = o.z * o.x;
+          for (int k = 1; k < a.team; k <<= 1) mean += __shfl_xor_sync(0xffffffffu, mean, k);
+          mean *= inv_c;
+          m2 = fmaf(o.z * (o.x - mean), o.x - mean, o.y);
+          for (int k = 1; k < a.team; k <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, k);
+        }
+        rstd = rsqrtf(fmaf(m2, inv_c, a.eps));
+        if (me.tw == 0 && (me.lane & (LANES - 1)) == 0 && live) {
+          a.mean[row] = mean;
+          a.rstd[row] = rstd;
+        }
+      } else {
+        mean = now.mean;
+        rstd = now.rstd;
+        if (a.team > 1 && r0 + AT_ONCE >= rows) named_barrier(1 + me.team, a.team * 32);
+      }
+      // The item is in registers, of every warp of the team: its stage takes the team's item after the
+      // ones already requested.
+      if (r0 + AT_ONCE >= rows) {
+        __syncwarp();
+        if (leader) norm_fetch<T, SRC, 0>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
+      }
+      const pair_t rs = both(rstd), off = both(-mean * rstd);
+      T* out = static_cast<T*>(a.y) + row * a.C + me.c0;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const bool in = FULL || (me.c0 + j * me.stride < a.C && live);
+        if (KIND == 1) {
+          const GroupScale gs = ckpt_group_scale<(LANES < 16 ? LANES : 16)>(v[j]);
+          if (in) {
+            *reinterpret_cast<uint2*>(a.codes_out + row * a.C + me.c0 + j * me.stride) = ckpt_codes(v[j], gs);
+            if ((me.lane & (LANES < 16 ? LANES - 1 : 15)) == 0)
+              a.scales_out[row * a.G + (me.c0 + j * me.stride) / CKPT_GROUP] = gs.scale;
+          }
+        }
+        if (in) {
+          pair_t o[4], gm[4], bt[4];
+          planes_load(gamma_at + j * me.stride * 2, plane, gm);
+          planes_load(beta_at + j * me.stride * 2, plane, bt);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = fma2(fma2(v[j][i], rs, off), gm[i], bt[i]);
+          store8(out + j * me.stride, o);
+        }
+      }
+    }
+    if (++s == a.stages) {
+      s = 0;
+      ph ^= 1;
+    }
+  }
+  if (leader) norm_drain(full, a.stages, requested, ctl);
+}
+
+// Backward.  A lane holds x, dY and gamma of its columns of the row between the sums and dX.  The
+// block writes one partial row of dgamma and dbeta at its end.
+template <typename T, int NV, int SRC, int FULL, int LANES, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
+  constexpr int XS = SRC ? 1 : static_cast<int>(sizeof(T)), DS = sizeof(T), AT_ONCE = 32 / LANES;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const Place<WARPS, LANES> me(a);
+  float* s_gamma = reinterpret_cast<float*>(smem + me.teams * a.stages * a.stage_bytes);
+  NormCtl* ctl = norm_setup(a, me.teams, reinterpret_cast<uint8_t*>(s_gamma + a.C));
+  uint8_t* ring = smem + me.team * a.stages * a.stage_bytes;
+  uint64_t* full = ctl->full + me.team * a.stages;
+  const int first = blockIdx.x * me.teams + me.team, step = gridDim.x * me.teams;
+  const bool leader = me.tw == 0 && me.lane == 0;
+  int requested = 0;
+  pdl_trigger();
+  pdl_wait();
+  if (leader)
+    for (int s = 0; s < a.stages; ++s)
+      norm_fetch<T, SRC, 1>(a, static_cast<int64_t>(first) + s * step, ring + s * a.stage_bytes, &full[s], ctl, requested);
+  planes_fill(s_gamma, a.gamma, a.C);
+  __syncthreads();
+  const uint32_t gamma_at = smem_u32(s_gamma) + me.c0 * 2, plane = a.C * 2, dy_off = a.R * a.C * XS;
+  pair_t dg[NV][4], db[NV][4];
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dg[j][i] = db[j][i] = 0.f;
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * teams + (a.team == 1 ? warp : 0); row < a.M;
-       row += static_cast<int64_t>(gridDim.x) * teams) {
-    const int64_t base = row * a.C;
-    float xh[NV][8], d[NV][8];
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    for (int i = 0; i < 4; ++i) dg[j][i] = db[j][i] = 0;
+  const float inv_c = 1.f / static_cast<float>(a.C);
+  int slot = 0, s = 0;
+  uint32_t ph = 0;
+  RowStats<NV, SRC> next = {}, now;
+  next.ask(a, static_cast<int64_t>(first) * a.R + me.sub, me.c0, me.stride);
+  for (int64_t item = first; item < a.items; item += step) {
+    const int64_t row0 = item * a.R;
+    const int rows = a.M - row0 < a.R ? static_cast<int>(a.M - row0) : a.R;
+    uint8_t* st = ring + s * a.stage_bytes;
+    norm_wait(&full[s], ph, ctl, a.status);
+    for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
+      const int r = r0 + me.sub;
+      const bool live = AT_ONCE == 1 || r < rows;
+      now = next;
+      next.ask(a, (r0 + AT_ONCE < rows ? row0 + r + AT_ONCE : (item + step) * a.R + me.sub), me.c0, me.stride);
+      const float mean = now.mean, rstd = now.rstd;
+      const uint32_t x_at = smem_u32(st) + (r * a.C + me.c0) * XS, d_at = smem_u32(st) + dy_off + (r * a.C + me.c0) * DS;
+      const pair_t rs = both(rstd), off = both(-mean * rstd);
+      pair_t x[NV][4], g[NV][4];
+      pair_t sg[2] = {0, 0}, sx[2] = {0, 0};      // sums of g and g xh
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = tl * 8 + j * stride;
-      Vec8<T> r;
-      r.zero();
-      if (c < a.C) r.load(static_cast<const T*>(a.dy) + base + c);
-      r.get(d[j]);
-      if (SRC == 0) {
-        r.zero();
-        if (c < a.C) r.load(static_cast<const T*>(a.x) + base + c);
-        r.get(xh[j]);
-      } else {
-        uint2 w = make_uint2(0u, 0u);
-        float s = 0.f;
-        if (c < a.C) {
-          w = *reinterpret_cast<const uint2*>(a.codes_in + base + c);
-          s = a.scales_in[row * a.G + c / CKPT_GROUP];
-        }
-        ckpt_values(w, s, xh[j]);
-      }
-    }
-    float2 s = make_float2(0.f, 0.f);      // sums of g and g xh
+      for (int j = 0; j < NV; ++j) {
+        if (FULL || (me.c0 + j * me.stride < a.C && live)) {
+          pair_t gm[4];
+          row_load<T, 0>(d_at + j * me.stride * DS, 0.f, g[j]);
+          row_load<T, SRC>(x_at + j * me.stride * XS, now.scale[j], x[j]);
+          planes_load(gamma_at + j * me.stride * 2, plane, gm);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = tl * 8 + j * stride;
-      if (c < a.C) {
-        float gm[8];
-        Vec8<float> p;
-        p.load(a.gamma + c);
-        p.get(gm);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          xh[j][i] = (xh[j][i] - mean) * rstd;
-          dg[j][i] = fmaf(d[j][i], xh[j][i], dg[j][i]);
-          db[j][i] += d[j][i];
-          d[j][i] *= gm[i];
-          s.x += d[j][i];
-          s.y = fmaf(d[j][i], xh[j][i], s.y);
+          for (int i = 0; i < 4; ++i) {
+            x[j][i] = fma2(x[j][i], rs, off);
+            dg[j][i] = fma2(g[j][i], x[j][i], dg[j][i]);
+            db[j][i] = add2(db[j][i], g[j][i]);
+            g[j][i] = mul2(g[j][i], gm[i]);
+            sg[i & 1] = add2(sg[i & 1], g[j][i]);
+            sx[i & 1] = fma2(g[j][i], x[j][i], sx[i & 1]);
+          }
         }
       }
-    }
-    s = team_sum(s, a.team, s_red, slot);
-    const float c1 = s.x * inv_c, c2 = s.y * inv_c;
+      float2 sum = make_float2(lanes_sum<LANES>(pair_sum(add2(sg[0], sg[1]))), lanes_sum<LANES>(pair_sum(add2(sx[0], sx[1]))));
+      if (a.team > 1) {
+        float4* red = ctl->red[slot] + me.team * a.team;
+        slot ^= 1;
+        if (me.lane == 0) red[me.tw] = make_float4(sum.x, sum.y, 0.f, 0.f);
+        named_barrier(1 + me.team, a.team * 32);
+        const float4 o = red[me.lane & (a.team - 1)];
+        sum = make_float2(o.x, o.y);
+        for (int k = 1; k < a.team; k <<= 1) {
+          sum.x += __shfl_xor_sync(0xffffffffu, sum.x, k);
+          sum.y += __shfl_xor_sync(0xffffffffu, sum.y, k);
+        }
+      }
+      // The item is in registers, of every warp of the team: its stage takes the next one.
+      if (r0 + AT_ONCE >= rows) {
+        __syncwarp();
+        if (leader) norm_fetch<T, SRC, 1>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
+      }
+      // dX = rstd g + xh * (-rstd mean(g xh)) - rstd mean(g)
+      const pair_t k1 = both(-rstd * sum.x * inv_c), k2 = both(-rstd * sum.y * inv_c);
+      T* out = static_cast<T*>(a.y) + (row0 + r) * a.C + me.c0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = tl * 8 + j * stride;
-      if (c < a.C) {
-        float o[8];
+      for (int j = 0; j < NV; ++j) {
+        if (FULL || (me.c0 + j * me.stride < a.C && live)) {
+          pair_t o[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = rstd * (d[j][i] - fmaf(xh[j][i], c2, c1));
-        store8(static_cast<T*>(a.y) + base + c, o);
+          for (int i = 0; i < 4; ++i) o[i] = fma2(g[j][i], rs, fma2(x[j][i], k2, k1));
+          store8(out + j * me.stride, o);
+        }
       }
     }
+    if (++s == a.stages) {
+      s = 0;
+      ph ^= 1;
+    }
+  }
+  if (leader) norm_drain(full, a.stages, requested, ctl);
+  // Join the rows of a warp, then the teams (their parts lie in the ring, which nothing writes any
+  // more), and write the block's part.
+  if (LANES < 32) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int o = LANES; o < 32; o <<= 1) {
+        dg[0][i] = add2(dg[0][i], __shfl_xor_sync(0xffffffffu, dg[0][i], o));
+        db[0][i] = add2(db[0][i], __shfl_xor_sync(0xffffffffu, db[0][i], o));
+      }
   }
   float* out = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.C;
-  if (teams == 1) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int c = tl * 8 + j * stride;
-      if (c < a.C) {
-        store8(out + c, dg[j]);
-        store8(out + a.C + c, db[j]);
-      }
-    }
-    return;
-  }
-  float* mine = s_part + static_cast<int64_t>(warp) * 2 * a.C;
+  float* mine = me.teams == 1 ? out : reinterpret_cast<float*>(smem) + me.team * 2 * a.C;
+  if (me.teams > 1) named_barrier(WHOLE_BLOCK, 32 * WARPS);
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int c = tl * 8 + j * stride;
-    if (c < a.C) {
+    const int c = me.c0 + j * me.stride;
+    if (FULL || (c < a.C && me.sub == 0)) {
       store8(mine + c, dg[j]);
       store8(mine + a.C + c, db[j]);
     }
   }
-  __syncthreads();
-  for (int c = threadIdx.x; c < 2 * a.C; c += blockDim.x) {
+  if (me.teams == 1) return;
+  named_barrier(WHOLE_BLOCK, 32 * WARPS);
+  for (int c = threadIdx.x; c < 2 * a.C; c += 32 * WARPS) {
     float t = 0.f;
-    for (int w = 0; w < teams; ++w) t += s_part[static_cast<int64_t>(w) * 2 * a.C + c];
+    for (int k = 0; k < me.teams; ++k) t += reinterpret_cast<const float*>(smem)[k * 2 * a.C + c];
     out[c] = t;
   }
 }
@@ -249,8 +451,10 @@ __global__ void __launch_bounds__(256) norm_reduce_kernel(const float* __restric
   const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + cx;
   float t = 0.f;
-  if (c < 2 * C)
+  if (c < 2 * C) {
+#pragma unroll 8
     for (int r = ry; r < parts; r += 8) t += part[static_cast<int64_t>(r) * 2 * C + c];
+  }
   s[ry][cx] = t;
   __syncthreads();
   if (ry == 0 && c < 2 * C) {
@@ -259,115 +463,172 @@ __global__ void __launch_bounds__(256) norm_reduce_kernel(const float* __restric
   }
 }
 
-// Warps per row and vectors per lane for a reach of `most` vectors.
+// Shape of a launch: lanes and warps per row (a power of two, so that teams fill the block), vectors per
+// lane, rows per item, ring.
 struct Shape {
-  int team, nv;
+  int warps, team, lanes, nv, R, stages, stage_bytes, items, grid;
+  size_t smem;
 };
-Shape row_shape(int64_t C, int most) {
+template <typename T, int SRC, int BWD>
+Shape norm_shape(int64_t M, int64_t C, int sm_count) {
   Shape s;
-  s.team = static_cast<int>(ceil_div(C, 256 * most));
+  const int c = static_cast<int>(C);
+  s.warps = !BWD ? FWD_WARPS : C <= 1024 * BWD_WARPS ? BWD_WARPS : WIDE_WARPS;
+  s.lanes = C <= 64 ? 8 : C <= 128 ? 16 : 32;
+  s.team = 1;
+  while (s.team < s.warps && static_cast<int64_t>(s.team) * 1024 < C) s.team *= 2;
+  const int extra = (BWD ? 1 : 2) * c * 4 + static_cast<int>(sizeof(NormCtl));      // gamma (and beta)
+  const int row_bytes = item_bytes<T, SRC, BWD>(1, c);
+  int room = 227 * 1024 - extra;
+  // the ring's share, or two rows of every team where that is more and there is room for it
+  const int want = BWD ? BWD_RING : FWD_RING, two = 2 * (s.warps / s.team) * row_bytes;
+  if (room > (want > two ? want : two)) room = want > two ? want : two;
+  while (s.team < s.warps && 2 * (s.warps / s.team) * row_bytes > room) s.team *= 2;
   s.nv = static_cast<int>(ceil_div(C, 256 * s.team));
+  const int teams = s.warps / s.team, at_once = 32 / s.lanes;
+  // short rows go several to a copy, as long as every team still gets one
+  int64_t R = ITEM_BYTES / (c * static_cast<int>(sizeof(T))) > 1 ? ITEM_BYTES / (c * static_cast<int>(sizeof(T))) : 1;
+  const int64_t even = ceil_div(M, static_cast<int64_t>(sm_count) * teams);
+  if (R > even) R = even;
+  s.R = static_cast<int>(round_up(R, at_once));
+  s.stage_bytes = item_bytes<T, SRC, BWD>(s.R, c);
+  s.stages = room / (teams * s.stage_bytes);
+  if (s.stages > RING_MAX) s.stages = RING_MAX;
+  s.items = static_cast<int>(ceil_div(M, s.R));
+  const int64_t blocks = ceil_div(s.items, teams);
+  s.grid = static_cast<int>(blocks < sm_count ? blocks : sm_count);
+  s.smem = static_cast<size_t>(teams) * s.stages * s.stage_bytes + extra;
+  // the backward joins its teams in the ring: [teams][2][C] floats
+  const size_t join = BWD && teams > 1 ? static_cast<size_t>(teams) * 2 * C * 4 : 0;
+  if (s.smem < join) s.smem = join;
   return s;
 }
 
-static const int FWD_NV = 4, BWD_NV = 4;
-
-template <typename T, int NV>
-void fwd_nv(const NormArgs& a, unsigned grid, unsigned block, cudaStream_t st) {
-  count_launches(1);
-  if (a.codes_in) launch_dependent(norm_fwd_kernel<T, NV, 1, 0>, grid, block, 0, st, 1, a);
-  else if (a.codes_out) launch_dependent(norm_fwd_kernel<T, NV, 0, 1>, grid, block, 0, st, 1, a);
-  else launch_dependent(norm_fwd_kernel<T, NV, 0, 0>, grid, block, 0, st, 1, a);
-}
-
-template <typename T>
-void fwd_t(const NormArgs& a, int nv, unsigned grid, unsigned block, cudaStream_t st) {
-  switch (nv) {
-    case 1: fwd_nv<T, 1>(a, grid, block, st); break;
-    case 2: fwd_nv<T, 2>(a, grid, block, st); break;
-    case 3: fwd_nv<T, 3>(a, grid, block, st); break;
-    default: fwd_nv<T, 4>(a, grid, block, st); break;
-  }
-}
-
-template <typename T, int NV>
-void bwd_nv(const NormArgs& a, unsigned grid, unsigned block, size_t smem, cudaStream_t st) {
-  count_launches(1);
-  if (a.codes_in) launch_dependent(norm_bwd_kernel<T, NV, 1>, grid, block, smem, st, 1, a);
-  else launch_dependent(norm_bwd_kernel<T, NV, 0>, grid, block, smem, st, 1, a);
-}
-
-template <typename T>
-void bwd_t(const NormArgs& a, int nv, unsigned grid, unsigned block, size_t smem, cudaStream_t st) {
-  switch (nv) {
-    case 1: bwd_nv<T, 1>(a, grid, block, smem, st); break;
-    case 2: bwd_nv<T, 2>(a, grid, block, smem, st); break;
-    case 3: bwd_nv<T, 3>(a, grid, block, smem, st); break;
-    default: bwd_nv<T, 4>(a, grid, block, smem, st); break;
-  }
-}
-
-struct BwdPlan {
-  int team, nv, warps, grid;
-};
-BwdPlan bwd_plan(int64_t M, int64_t C, int sm_count) {
-  const Shape s = row_shape(C, BWD_NV);
-  BwdPlan p;
-  p.team = s.team; p.nv = s.nv;
-  p.warps = s.team == 1 ? 4 : s.team;
-  const int64_t teams = s.team == 1 ? 4 : 1;
-  const int64_t need = ceil_div(M, teams), cap = static_cast<int64_t>(sm_count) * (s.team <= 4 ? 2 : 1);
-  p.grid = static_cast<int>(need < cap ? need : cap);
-  return p;
-}
-
-NormArgs norm_args(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, int team) {
+NormArgs norm_args(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const Shape& s, int* status) {
   NormArgs a = {};
   a.x = x;
   if (in) { a.codes_in = in->codes; a.scales_in = in->scales; }
   a.M = M;
   a.C = static_cast<int>(C);
   a.G = static_cast<int>(ckpt_groups(C));
-  a.team = team;
+  a.team = s.team; a.R = s.R; a.stages = s.stages; a.stage_bytes = s.stage_bytes; a.items = s.items;
+  a.status = status;
   return a;
+}
+
+// The kernels of a shape.  Rows of up to 128 columns have 8 or 16 lanes to a row and one vector per lane;
+// FULL kernels run where every lane's columns exist; the backward has 8 warps, 16 beyond 8192 columns.
+typedef void (*NormKernel)(NormArgs);
+template <typename T, int NV, int KIND>
+NormKernel fwd_kernel_nv(bool full) {
+  return full ? norm_fwd_kernel<T, NV, KIND, 1, 32> : norm_fwd_kernel<T, NV, KIND, 0, 32>;
+}
+template <typename T, int KIND>
+NormKernel fwd_kernel(int lanes, int nv, bool full) {
+  if (lanes == 8) return norm_fwd_kernel<T, 1, KIND, 0, 8>;
+  if (lanes == 16) return norm_fwd_kernel<T, 1, KIND, 0, 16>;
+  switch (nv) {
+    case 1: return fwd_kernel_nv<T, 1, KIND>(full);
+    case 2: return fwd_kernel_nv<T, 2, KIND>(full);
+    case 3: return fwd_kernel_nv<T, 3, KIND>(full);
+    default: return fwd_kernel_nv<T, 4, KIND>(full);
+  }
+}
+template <typename T, int NV, int SRC, int WARPS>
+NormKernel bwd_kernel_nv(bool full) {
+  return full ? norm_bwd_kernel<T, NV, SRC, 1, 32, WARPS> : norm_bwd_kernel<T, NV, SRC, 0, 32, WARPS>;
+}
+template <typename T, int SRC>
+NormKernel bwd_kernel(int warps, int lanes, int nv, bool full) {
+  if (warps == WIDE_WARPS) return nv == 3 ? bwd_kernel_nv<T, 3, SRC, WIDE_WARPS>(full) : bwd_kernel_nv<T, 4, SRC, WIDE_WARPS>(full);
+  if (lanes == 8) return norm_bwd_kernel<T, 1, SRC, 0, 8, BWD_WARPS>;
+  if (lanes == 16) return norm_bwd_kernel<T, 1, SRC, 0, 16, BWD_WARPS>;
+  switch (nv) {
+    case 1: return bwd_kernel_nv<T, 1, SRC, BWD_WARPS>(full);
+    case 2: return bwd_kernel_nv<T, 2, SRC, BWD_WARPS>(full);
+    case 3: return bwd_kernel_nv<T, 3, SRC, BWD_WARPS>(full);
+    default: return bwd_kernel_nv<T, 4, SRC, BWD_WARPS>(full);
+  }
+}
+
+bool launch_norm(NormKernel k, const NormArgs& a, const Shape& s, cudaStream_t st) {
+  return launch_dependent(k, static_cast<unsigned>(s.grid), 32u * s.warps, s.smem, st, 1, a) == cudaSuccess;
+}
+
+template <typename T>
+int fwd_t(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma, const float* beta, float eps,
+          void* y, float* mean, float* rstd, const efqat_ckpt* out, int* status, int sm_count, cudaStream_t st) {
+  const Shape s = in ? norm_shape<T, 1, 0>(M, C, sm_count) : norm_shape<T, 0, 0>(M, C, sm_count);
+  NormArgs a = norm_args(x, in, M, C, s, status);
+  a.gamma = gamma; a.beta = beta; a.eps = eps;
+  a.y = y; a.mean = mean; a.rstd = rstd;
+  if (out) { a.codes_out = out->codes; a.scales_out = out->scales; }
+  count_launches(1);
+  const bool full = C == 256 * s.nv * s.team;
+  const bool ok = launch_norm(in    ? fwd_kernel<T, 2>(s.lanes, s.nv, full)
+                              : out ? fwd_kernel<T, 1>(s.lanes, s.nv, full)
+                                    : fwd_kernel<T, 0>(s.lanes, s.nv, full), a, s, st);
+  return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
+}
+
+template <typename T>
+int bwd_t(const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
+          const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta, float* part, int* status,
+          int sm_count, cudaStream_t st) {
+  const Shape s = in ? norm_shape<T, 1, 1>(M, C, sm_count) : norm_shape<T, 0, 1>(M, C, sm_count);
+  NormArgs a = norm_args(x, in, M, C, s, status);
+  a.dy = dy; a.gamma = gamma;
+  a.y = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
+  a.part = part;
+  count_launches(2);
+  const bool full = C == 256 * s.nv * s.team;
+  bool ok = launch_norm(in ? bwd_kernel<T, 1>(s.warps, s.lanes, s.nv, full) : bwd_kernel<T, 0>(s.warps, s.lanes, s.nv, full),
+                        a, s, st);
+  ok = ok && launch_dependent(norm_reduce_kernel, static_cast<unsigned>(ceil_div(2 * C, 32)), 256, 0, st, 1,
+                              static_cast<const float*>(part), s.grid, static_cast<int>(C), dgamma, dbeta) == cudaSuccess;
+  return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
+}
+
+bool big_smem(NormKernel k) {
+  return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) == cudaSuccess;
+}
+template <typename T>
+bool allow_rings() {
+  bool ok = true;
+  for (int lanes = 8; lanes <= 32; lanes *= 2)
+    for (int nv = 1; nv <= (lanes == 32 ? 4 : 1); ++nv)
+      for (int full = 0; full < (lanes == 32 ? 2 : 1); ++full) {
+        ok = ok && big_smem(fwd_kernel<T, 0>(lanes, nv, full)) && big_smem(fwd_kernel<T, 1>(lanes, nv, full)) &&
+             big_smem(fwd_kernel<T, 2>(lanes, nv, full));
+        ok = ok && big_smem(bwd_kernel<T, 0>(BWD_WARPS, lanes, nv, full)) && big_smem(bwd_kernel<T, 1>(BWD_WARPS, lanes, nv, full));
+        if (nv >= 3)
+          ok = ok && big_smem(bwd_kernel<T, 0>(WIDE_WARPS, lanes, nv, full)) && big_smem(bwd_kernel<T, 1>(WIDE_WARPS, lanes, nv, full));
+      }
+  return ok;
 }
 
 }  // namespace
 
+int norm_init() { return allow_rings<bf16>() && allow_rings<float>() ? EFQAT_OK : EFQAT_ERR_CUDA; }
+
+// One part per block; the grid never has more blocks than rows or SMs.
 size_t layer_norm_workspace_bytes(int64_t M, int64_t C, int sm_count) {
-  return M > 0 ? static_cast<size_t>(bwd_plan(M, C, sm_count).grid) * 2 * C * 4 : 0;
+  return static_cast<size_t>(M < sm_count ? M : sm_count) * 2 * C * 4;
 }
 
-void launch_norm_fwd(int dtype, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
-                     const float* beta, float eps, void* y, float* mean, float* rstd, const efqat_ckpt* out,
-                     int sm_count, cudaStream_t st) {
-  const Shape s = row_shape(C, FWD_NV);
-  NormArgs a = norm_args(x, in, M, C, s.team);
-  a.gamma = gamma; a.beta = beta; a.eps = eps;
-  a.y = y; a.mean = mean; a.rstd = rstd;
-  if (out) { a.codes_out = out->codes; a.scales_out = out->scales; }
-  const int warps = s.team == 1 ? 4 : s.team;
-  const int64_t need = ceil_div(M, s.team == 1 ? 4 : 1);
-  const int64_t cap = static_cast<int64_t>(sm_count) * (32 / warps > 0 ? 32 / warps : 1);
-  const unsigned grid = static_cast<unsigned>(need < cap ? need : cap);
-  if (dtype == EFQAT_BF16) fwd_t<bf16>(a, s.nv, grid, warps * 32, st);
-  else fwd_t<float>(a, s.nv, grid, warps * 32, st);
+int launch_norm_fwd(int dtype, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
+                    const float* beta, float eps, void* y, float* mean, float* rstd, const efqat_ckpt* out,
+                    int* status, int sm_count, cudaStream_t st) {
+  return dtype == EFQAT_BF16 ? fwd_t<bf16>(x, in, M, C, gamma, beta, eps, y, mean, rstd, out, status, sm_count, st)
+                             : fwd_t<float>(x, in, M, C, gamma, beta, eps, y, mean, rstd, out, status, sm_count, st);
 }
 
-void launch_norm_bwd(int dtype, const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C,
-                     const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta,
-                     float* part, int sm_count, cudaStream_t st) {
-  const BwdPlan p = bwd_plan(M, C, sm_count);
-  NormArgs a = norm_args(x, in, M, C, p.team);
-  a.dy = dy; a.gamma = gamma;
-  a.y = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
-  a.part = part;
-  const size_t smem = p.team == 1 ? static_cast<size_t>(p.warps) * 2 * C * 4 : 0;     // at most 4 * 2 * 1024 * 4 = 32 KB
-  if (dtype == EFQAT_BF16) bwd_t<bf16>(a, p.nv, p.grid, p.warps * 32, smem, st);
-  else bwd_t<float>(a, p.nv, p.grid, p.warps * 32, smem, st);
-  count_launches(1);
-  launch_dependent(norm_reduce_kernel, static_cast<unsigned>(ceil_div(2 * C, 32)), 256, 0, st, 1,
-                   static_cast<const float*>(part), p.grid, static_cast<int>(C), dgamma, dbeta);
+int launch_norm_bwd(int dtype, const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C,
+                    const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta,
+                    float* part, int* status, int sm_count, cudaStream_t st) {
+  return dtype == EFQAT_BF16
+             ? bwd_t<bf16>(dy, x, in, M, C, gamma, mean, rstd, dx, dgamma, dbeta, part, status, sm_count, st)
+             : bwd_t<float>(dy, x, in, M, C, gamma, mean, rstd, dx, dgamma, dbeta, part, status, sm_count, st);
 }
 
 }  // namespace efqat

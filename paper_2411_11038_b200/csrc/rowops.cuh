@@ -5,6 +5,7 @@
 // 8 registers and 4 shuffles, its codes leave as one 8-byte store per lane.
 #pragma once
 #include "internal.h"
+#include "ptx.cuh"
 
 namespace efqat {
 
@@ -12,7 +13,49 @@ static const int CKPT_GROUP = 128;
 
 __host__ __device__ inline int64_t ckpt_groups(int64_t C) { return ceil_div(C, CKPT_GROUP); }
 
-// 8 consecutive elements <-> fp32 registers (16-byte accesses).
+// Two fp32 values in one aligned register pair: the packed instructions do both for one issue slot.
+// Kept as one 64-bit value throughout, so that no moves are spent on joining and splitting halves.
+typedef unsigned long long pair_t;
+__device__ __forceinline__ pair_t pair_of(uint32_t lo, uint32_t hi) {
+  pair_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ pair_t pair_of(float lo, float hi) { return pair_of(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ pair_t both(float v) { return pair_of(v, v); }
+__device__ __forceinline__ float2 halves(pair_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
+  pair_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
+  pair_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
+  pair_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// 8 consecutive elements as they lie in memory <-> four pairs of fp32 (16-byte accesses).
+__device__ __forceinline__ void unpack8(const uint4& r, pair_t (&v)[4]) {      // 8 bf16
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pair_of(w[i] << 16, w[i] & 0xffff0000u);
+}
+__device__ __forceinline__ void unpack8(const uint4& r, const uint4& q, pair_t (&v)[4]) {      // 8 fp32
+  v[0] = pair_of(r.x, r.y);
+  v[1] = pair_of(r.z, r.w);
+  v[2] = pair_of(q.x, q.y);
+  v[3] = pair_of(q.z, q.w);
+}
 template <typename T>
 struct Vec8;
 template <>
@@ -20,54 +63,46 @@ struct Vec8<bf16> {
   uint4 r;
   __device__ __forceinline__ void load(const bf16* p) { r = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void zero() { r = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
+  __device__ __forceinline__ void get(pair_t (&v)[4]) const { unpack8(r, v); }
 };
 template <>
 struct Vec8<float> {
-  float4 a, b;
+  uint4 r, q;
   __device__ __forceinline__ void load(const float* p) {
-    a = reinterpret_cast<const float4*>(p)[0];
-    b = reinterpret_cast<const float4*>(p)[1];
+    r = reinterpret_cast<const uint4*>(p)[0];
+    q = reinterpret_cast<const uint4*>(p)[1];
   }
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
+  __device__ __forceinline__ void zero() { r = q = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(pair_t (&v)[4]) const { unpack8(r, q, v); }
 };
 
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+__device__ __forceinline__ uint32_t pack_bf16(pair_t v) {
+  const float2 f = halves(v);
+  const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
-  *reinterpret_cast<uint4*>(p) =
-      make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+__device__ __forceinline__ void store8(bf16* p, const pair_t (&v)[4]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0]), pack_bf16(v[1]), pack_bf16(v[2]), pack_bf16(v[3]));
 }
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+__device__ __forceinline__ void store8(float* p, const pair_t (&v)[4]) {
+  reinterpret_cast<ulonglong2*>(p)[0] = make_ulonglong2(v[0], v[1]);
+  reinterpret_cast<ulonglong2*>(p)[1] = make_ulonglong2(v[2], v[3]);
 }
 
-// Scale and multiplier of the group that this lane's 16-lane half of the warp holds.  The largest
-// magnitude is taken over the bit patterns, where infinity and NaN rank above every finite value.
-// Every lane of the warp has to take part.
+// Scale and multiplier of the group that LANES neighbouring lanes hold (16, or 8 for rows of up to 64
+// columns).  The largest magnitude is taken over the bit patterns, where infinity and NaN rank above
+// every finite value.  Every lane of the warp has to take part.
 struct GroupScale {
   float scale, factor;     // value of one code step; multiplier that decides the codes
 };
-__device__ __forceinline__ GroupScale ckpt_group_scale(const float (&v)[8]) {
+template <int LANES = 16>
+__device__ __forceinline__ GroupScale ckpt_group_scale(const pair_t (&v)[4]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  for (int i = 0; i < 4; ++i)
+    top = max(top, max(static_cast<uint32_t>(v[i]) & 0x7fffffffu, static_cast<uint32_t>(v[i] >> 32) & 0x7fffffffu));
 #pragma unroll
-  for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   const float a = __uint_as_float(top);
   GroupScale g;
   if (top >= 0x7f800000u) {
@@ -85,10 +120,16 @@ __device__ __forceinline__ GroupScale ckpt_group_scale(const float (&v)[8]) {
 
 // The 8 codes of a lane as two words.  Adding 1.5 * 2^23 rounds to nearest-even and leaves the code
 // in the low byte of the sum's bit pattern (two's complement), so no conversion instruction is used.
-__device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], const GroupScale& g) {
+__device__ __forceinline__ uint2 ckpt_codes(const pair_t (&v)[4], const GroupScale& g) {
   uint32_t c[8];
+  const pair_t f = both(g.factor);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], g.factor), 12582912.f));
+  for (int i = 0; i < 4; ++i) {
+    // the product is rounded before the sum (one by one: a packed product and sum came out fused)
+    const float2 q = halves(mul2(v[i], f));
+    c[2 * i] = __float_as_uint(__fadd_rn(q.x, 12582912.f));
+    c[2 * i + 1] = __float_as_uint(__fadd_rn(q.y, 12582912.f));
+  }
   uint2 w;
   w.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
   w.y = __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410);
@@ -98,11 +139,16 @@ __device__ __forceinline__ uint2 ckpt_codes(const float (&v)[8], const GroupScal
 
 // The values that 8 codes stand for.  A code byte with its top bit flipped, placed in the mantissa
 // of 2^23, is 2^23 + 128 + code: one subtraction instead of an integer conversion.
-__device__ __forceinline__ void ckpt_values(uint2 w, float scale, float (&v)[8]) {
+__device__ __forceinline__ void ckpt_values(uint2 w, float scale, pair_t (&v)[4]) {
   const uint32_t x[2] = {w.x ^ 0x80808080u, w.y ^ 0x80808080u};
+  const pair_t off = both(-8388736.f), sc = both(scale);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    v[i] = __fmul_rn(__uint_as_float(__byte_perm(x[i >> 2], 0x4b000000u, 0x7440 | (i & 3))) - 8388736.f, scale);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = x[i >> 1];
+    const pair_t q = pair_of(__byte_perm(u, 0x4b000000u, (i & 1) ? 0x7442 : 0x7440),
+                             __byte_perm(u, 0x4b000000u, (i & 1) ? 0x7443 : 0x7441));
+    v[i] = mul2(add2(q, off), sc);
+  }
 }
 
 }  // namespace efqat
