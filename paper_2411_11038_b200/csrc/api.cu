@@ -1079,7 +1079,7 @@ static int rows_impl(efqat_ctx* ctx, int dtype, int act, const void* x, const ef
                      int64_t C, void* y, const efqat_ckpt* out, efqat_stream_t stream) {
   if (M == 0) return EFQAT_OK;
   Entered guard(ctx);
-  launch_ckpt(dtype, act, x, in, dY, M, C, y, out, ctx->sm_count, stream);
+  launch_ckpt(dtype, act, x, in, dY, M, C, y, out, stream);
   return last_error();
 }
 

@@ -9,6 +9,11 @@
 // error of erf at most 1.5e-7).  The slope Phi(x) + x e / sqrt(2 pi) needs the same exponential, so
 // either direction costs two special-function operations per element (a reciprocal and a power of
 // two); the rest goes through the packed fp32 instructions, two elements to an issue slot.
+//
+// HBM-bound in principle (4 to 5 bytes per element and pass), but at 23 bytes per cycle and SM an
+// element may cost no more than 22 to 28 issue slots of a lane.  Hence 16 elements per lane: a group
+// is 8 lanes, its scale costs 3 shuffles and two divisions per 16 elements, and every access is one
+// of 32 bytes (16 for the codes).
 #include "rowops.cuh"
 
 namespace efqat {
@@ -16,6 +21,8 @@ namespace efqat {
 namespace {
 
 enum { ACT_NONE = 0, ACT_GELU = 1, ACT_GELU_BWD = 2 };
+
+static const int BLOCK = 256;
 
 __device__ __forceinline__ float rcp_approx(float x) {
   float r;
@@ -59,119 +66,190 @@ struct RowArgs {
   const void* x; const int8_t* codes_in; const float* scales_in;
   const void* dy;
   void* y; int8_t* codes_out; float* scales_out;
+  int64_t count;            // elements
   uint32_t C, G, groups;    // row length, groups per row, groups in all
+  int wide;                 // x, dy and y are 32-byte aligned
 };
 
-// One warp per pair of groups (16 lanes a group), UNROLL pairs in flight.  SRC: 0 x itself, 1 its
-// checkpoint.  HBM-bound: every tensor is touched once, with 16-byte (codes: 8-byte) accesses.
+// 32 bytes of 16 (bf16) or 8 (fp32) elements.
+__device__ __forceinline__ void load32(const void* p, int wide, uint4& a, uint4& b) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                 : "l"(p));
+  } else {
+    a = reinterpret_cast<const uint4*>(p)[0];
+    b = reinterpret_cast<const uint4*>(p)[1];
+  }
+}
+__device__ __forceinline__ void store32(void* p, int wide, const uint4& a, const uint4& b) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z),
+                 "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = a;
+    reinterpret_cast<uint4*>(p)[1] = b;
+  }
+}
+
+// 16 consecutive elements of a lane.
+template <typename T>
+struct Vec16;
+template <>
+struct Vec16<bf16> {
+  uint4 r[2];
+  __device__ __forceinline__ void load(const void* base, int64_t at, int wide) {
+    load32(static_cast<const bf16*>(base) + at, wide, r[0], r[1]);
+  }
+  __device__ __forceinline__ void zero() { r[0] = r[1] = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(pair_t (&v)[8]) const {
+    unpack8(r[0], *reinterpret_cast<pair_t(*)[4]>(&v[0]));
+    unpack8(r[1], *reinterpret_cast<pair_t(*)[4]>(&v[4]));
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t at, int wide, const pair_t (&v)[8]) {
+    store32(static_cast<bf16*>(base) + at, wide,
+            make_uint4(pack_bf16(v[0]), pack_bf16(v[1]), pack_bf16(v[2]), pack_bf16(v[3])),
+            make_uint4(pack_bf16(v[4]), pack_bf16(v[5]), pack_bf16(v[6]), pack_bf16(v[7])));
+  }
+};
+__device__ __forceinline__ uint4 quad(pair_t a, pair_t b) {
+  return make_uint4(static_cast<uint32_t>(a), static_cast<uint32_t>(a >> 32), static_cast<uint32_t>(b),
+                    static_cast<uint32_t>(b >> 32));
+}
+template <>
+struct Vec16<float> {
+  uint4 r[4];
+  __device__ __forceinline__ void load(const void* base, int64_t at, int wide) {
+    load32(static_cast<const float*>(base) + at, wide, r[0], r[1]);
+    load32(static_cast<const float*>(base) + at + 8, wide, r[2], r[3]);
+  }
+  __device__ __forceinline__ void zero() { r[0] = r[1] = r[2] = r[3] = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void get(pair_t (&v)[8]) const {
+    unpack8(r[0], r[1], *reinterpret_cast<pair_t(*)[4]>(&v[0]));
+    unpack8(r[2], r[3], *reinterpret_cast<pair_t(*)[4]>(&v[4]));
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t at, int wide, const pair_t (&v)[8]) {
+    store32(static_cast<float*>(base) + at, wide, quad(v[0], v[1]), quad(v[2], v[3]));
+    store32(static_cast<float*>(base) + at + 8, wide, quad(v[4], v[5]), quad(v[6], v[7]));
+  }
+};
+
+template <int ACT>
+__device__ __forceinline__ void activate(const pair_t (&v)[8], const pair_t (&d)[8], pair_t (&o)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = ACT == ACT_GELU ? gelu2(v[i]) : ACT == ACT_GELU_BWD ? mul2(d[i], gelu_slope2(v[i])) : v[i];
+}
+
+// With a checkpoint (CK): 8 lanes a group, 4 groups a warp.  SRC: 0 x itself, 1 its checkpoint.  Without
+// one the tensor is a flat array of 16-element pieces, the last of which may be half.  One piece per
+// thread at 32 registers, 64 warps an SM: 16384 x 4096 bf16, GELU with its checkpoint 52 us, its
+// backward 53 us, store and load 32 us (97 to 99 % of the measured copy bandwidth); two pieces per thread
+// at half the occupancy took 61 / 66 / 36 / 35 us, a loop over a fixed grid 10 to 20 % longer.
 template <typename T, int SRC, int ACT, int SAVE>
-__global__ void __launch_bounds__(256) ckpt_kernel(RowArgs a) {
-  constexpr int UNROLL = 2;
+__global__ void __launch_bounds__(BLOCK, 8) ckpt_kernel(RowArgs a) {
+  constexpr bool CK = SRC || SAVE;
   pdl_trigger();
   pdl_wait();
-  const uint32_t half = (blockIdx.x * 256u + threadIdx.x) >> 4;     // half-warps: one group each
-  const uint32_t halves = gridDim.x * 16u;
-  const int l16 = threadIdx.x & 15;
-  const bool ragged = (a.C % CKPT_GROUP) != 0;
-  // (whole warps stay in the loop together: the group maximum is a shuffle over the warp)
-  for (uint32_t g0 = half & ~1u; g0 < a.groups; g0 += halves * UNROLL) {
-    Vec8<T> xv[UNROLL], dv[UNROLL];
-    uint2 cv[UNROLL];
-    float sc[UNROLL];
-    int64_t at[UNROLL];
-    bool ok[UNROLL];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const uint32_t g = g0 + (half & 1u) + u * halves;
-      ok[u] = g < a.groups;
-      if (ragged) {
-        const uint32_t row = g / a.G, col = (g - row * a.G) * CKPT_GROUP + l16 * 8;
-        ok[u] = ok[u] && col < a.C;
-        at[u] = static_cast<int64_t>(row) * a.C + col;
-      } else {
-        at[u] = static_cast<int64_t>(g) * CKPT_GROUP + l16 * 8;
-      }
-      xv[u].zero();
-      if (SRC == 0) {
-        if (ok[u]) xv[u].load(static_cast<const T*>(a.x) + at[u]);
-      } else {
-        cv[u] = make_uint2(0u, 0u);
-        sc[u] = 0.f;
-        if (ok[u]) {
-          cv[u] = *reinterpret_cast<const uint2*>(a.codes_in + at[u]);
-          sc[u] = a.scales_in[g];
-        }
-      }
-      if (ACT == ACT_GELU_BWD) {
-        dv[u].zero();
-        if (ok[u]) dv[u].load(static_cast<const T*>(a.dy) + at[u]);
-      }
+  const uint32_t lane8 = threadIdx.x & 7, g = blockIdx.x * (BLOCK / 8) + (threadIdx.x >> 3);
+  bool ok = g < a.groups;
+  int64_t at = static_cast<int64_t>(g) * CKPT_GROUP + lane8 * 16;
+  if (!CK) {
+    ok = at + 16 <= a.count;
+  } else if (a.C % CKPT_GROUP != 0) {
+    const uint32_t row = g / a.G, col = (g - row * a.G) * CKPT_GROUP + lane8 * 16;
+    ok = ok && col < a.C;
+    at = static_cast<int64_t>(row) * a.C + col;
+  }
+  Vec16<T> xv, dv;
+  pair_t v[8], d[8] = {}, o[8];
+  uint4 cv = make_uint4(0u, 0u, 0u, 0u);
+  float sc = 0.f;
+  xv.zero();
+  dv.zero();
+  if (ok) {
+    if (SRC == 0) {
+      xv.load(a.x, at, a.wide);
+    } else {
+      cv = *reinterpret_cast<const uint4*>(a.codes_in + at);
+      sc = a.scales_in[g];
     }
+    if (ACT == ACT_GELU_BWD) dv.load(a.dy, at, a.wide);
+  }
+  if (SRC == 0) {
+    xv.get(v);
+  } else {
+    ckpt_values(make_uint2(cv.x, cv.y), sc, *reinterpret_cast<pair_t(*)[4]>(&v[0]));
+    ckpt_values(make_uint2(cv.z, cv.w), sc, *reinterpret_cast<pair_t(*)[4]>(&v[4]));
+  }
+  if (SAVE) {      // (no lane has left: the maximum is a shuffle over the warp)
+    uint32_t top = max(ckpt_top(xv.r[0], T()), ckpt_top(xv.r[1], T()));
+    if (sizeof(T) == 4) top = max(top, max(ckpt_top(xv.r[sizeof(T) / 2], T()), ckpt_top(xv.r[sizeof(T) - 1], T())));
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      const uint32_t g = g0 + (half & 1u) + u * halves;
-      pair_t v[4];
-      if (SRC == 0) xv[u].get(v); else ckpt_values(cv[u], sc[u], v);
-      if (SAVE) {
-        const GroupScale gs = ckpt_group_scale(v);
-        if (ok[u]) {
-          *reinterpret_cast<uint2*>(a.codes_out + at[u]) = ckpt_codes(v, gs);
-          if (l16 == 0) a.scales_out[g] = gs.scale;
-        }
-      }
-      if (SAVE && ACT == ACT_NONE) continue;
-      pair_t o[4];
-      if (ACT == ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = v[i];
-      } else if (ACT == ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = gelu2(v[i]);
-      } else {
-        pair_t d[4];
-        dv[u].get(d);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = mul2(d[i], gelu_slope2(v[i]));
-      }
-      if (ok[u]) store8(static_cast<T*>(a.y) + at[u], o);
+    for (int s = 4; s > 0; s >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, s));
+    const GroupScale gs = ckpt_scale_of(top);
+    if (ok) {
+      const uint2 lo = ckpt_codes(*reinterpret_cast<pair_t(*)[4]>(&v[0]), gs);
+      const uint2 hi = ckpt_codes(*reinterpret_cast<pair_t(*)[4]>(&v[4]), gs);
+      *reinterpret_cast<uint4*>(a.codes_out + at) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      if (lane8 == 0) a.scales_out[g] = gs.scale;
     }
+  }
+  if (!(SAVE && ACT == ACT_NONE)) {
+    if (ACT == ACT_GELU_BWD) dv.get(d);
+    activate<ACT>(v, d, o);
+    if (ok) Vec16<T>::store(a.y, at, a.wide, o);
+  }
+  // a flat array's last 8 elements
+  if (!CK && (a.count & 15) && blockIdx.x == 0 && threadIdx.x == 0) {
+    const int64_t at = a.count - 8;
+    Vec8<T> x8, d8;
+    pair_t v[8] = {}, d[8] = {}, o[8];
+    x8.load(static_cast<const T*>(a.x) + at);
+    x8.get(*reinterpret_cast<pair_t(*)[4]>(&v[0]));
+    if (ACT == ACT_GELU_BWD) {
+      d8.load(static_cast<const T*>(a.dy) + at);
+      d8.get(*reinterpret_cast<pair_t(*)[4]>(&d[0]));
+    }
+    activate<ACT>(v, d, o);
+    store8(static_cast<T*>(a.y) + at, *reinterpret_cast<pair_t(*)[4]>(&o[0]));
   }
 }
 
 template <typename T, int SRC, int ACT, int SAVE>
-void launch(const RowArgs& a, int sm_count, cudaStream_t st) {
-  const int64_t blocks = ceil_div(a.groups, 16);
-  const int64_t cap = static_cast<int64_t>(sm_count) * 8;
+void launch(const RowArgs& a, cudaStream_t st) {
   count_launches(1);
-  launch_dependent(ckpt_kernel<T, SRC, ACT, SAVE>, static_cast<unsigned>(blocks < cap ? blocks : cap), 256, 0, st, 1, a);
+  launch_dependent(ckpt_kernel<T, SRC, ACT, SAVE>, static_cast<unsigned>(ceil_div(a.groups, BLOCK / 8)), BLOCK, 0, st, 1, a);
 }
 
 template <typename T>
-void dispatch(const RowArgs& a, int act, int sm_count, cudaStream_t st) {
+void dispatch(const RowArgs& a, int act, cudaStream_t st) {
   const bool src = a.codes_in != nullptr, save = a.codes_out != nullptr;
   if (act == ACT_GELU_BWD) {
-    if (src) launch<T, 1, ACT_GELU_BWD, 0>(a, sm_count, st); else launch<T, 0, ACT_GELU_BWD, 0>(a, sm_count, st);
+    if (src) launch<T, 1, ACT_GELU_BWD, 0>(a, st); else launch<T, 0, ACT_GELU_BWD, 0>(a, st);
   } else if (act == ACT_GELU) {
-    if (src) launch<T, 1, ACT_GELU, 0>(a, sm_count, st);
-    else if (save) launch<T, 0, ACT_GELU, 1>(a, sm_count, st);
-    else launch<T, 0, ACT_GELU, 0>(a, sm_count, st);
+    if (src) launch<T, 1, ACT_GELU, 0>(a, st);
+    else if (save) launch<T, 0, ACT_GELU, 1>(a, st);
+    else launch<T, 0, ACT_GELU, 0>(a, st);
   } else {
-    if (src) launch<T, 1, ACT_NONE, 0>(a, sm_count, st); else launch<T, 0, ACT_NONE, 1>(a, sm_count, st);
+    if (src) launch<T, 1, ACT_NONE, 0>(a, st); else launch<T, 0, ACT_NONE, 1>(a, st);
   }
 }
 
 }  // namespace
 
 void launch_ckpt(int dtype, int act, const void* x, const efqat_ckpt* in, const void* dy, int64_t M, int64_t C,
-                 void* y, const efqat_ckpt* out, int sm_count, cudaStream_t st) {
+                 void* y, const efqat_ckpt* out, cudaStream_t st) {
   RowArgs a = {};
   a.x = x; a.dy = dy; a.y = y;
   if (in) { a.codes_in = in->codes; a.scales_in = in->scales; }
   if (out) { a.codes_out = out->codes; a.scales_out = out->scales; }
+  a.count = M * C;
   a.C = static_cast<uint32_t>(C);
   a.G = static_cast<uint32_t>(ckpt_groups(C));
-  a.groups = static_cast<uint32_t>(M * ckpt_groups(C));
-  if (dtype == EFQAT_BF16) dispatch<bf16>(a, act, sm_count, st); else dispatch<float>(a, act, sm_count, st);
+  a.groups = static_cast<uint32_t>(in || out ? M * ckpt_groups(C) : ceil_div(a.count, CKPT_GROUP));
+  a.wide = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(dy) | reinterpret_cast<uintptr_t>(y)) & 31) == 0;
+  if (dtype == EFQAT_BF16) dispatch<bf16>(a, act, st); else dispatch<float>(a, act, st);
 }
 
 }  // namespace efqat

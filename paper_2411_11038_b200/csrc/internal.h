@@ -108,7 +108,7 @@ void launch_log2_init(const float* s, float* theta, int64_t n, int* status, cuda
 // One streaming pass over [M,C].  act: 0 none (x given: store into `out`; `in` given: load into y),
 // 1 GELU (optionally also storing x into `out`), 2 GELU backward (dy).  Exactly one of x, in.
 void launch_ckpt(int dtype, int act, const void* x, const efqat_ckpt* in, const void* dy, int64_t M, int64_t C,
-                 void* y, const efqat_ckpt* out, int sm_count, cudaStream_t st);
+                 void* y, const efqat_ckpt* out, cudaStream_t st);
 
 // ---- norm.cu ------------------------------------------------------------------------
 // in given: y from the checkpoint and the given mean / rstd; else mean and rstd are written.

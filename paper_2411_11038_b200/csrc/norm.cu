@@ -30,7 +30,7 @@ static const int ITEM_BYTES = 2048;           // short rows: as many to a copy a
 // Warps of a block and bytes of its ring: the forward hides its row's chain of reductions behind other
 // rows, the backward wants the registers of few warps (it holds a row's x and dY and its 64 sums).
 static const int FWD_WARPS = 16, BWD_WARPS = 8, WIDE_WARPS = 16;
-static const int FWD_RING = 64 * 1024, BWD_RING = 160 * 1024;
+static const int FWD_RING = 64 * 1024, BWD_RING = 112 * 1024;
 
 struct NormArgs {
   const void* x; const int8_t* codes_in; const float* scales_in;
@@ -110,6 +110,18 @@ __device__ __forceinline__ void row_load(uint32_t addr, float scale, pair_t (&v)
   else if (sizeof(T) == 2) unpack8(lds128(addr), v);
   else unpack8(lds128(addr), lds128(addr + 16), v);
 }
+// ... and their largest magnitude.
+template <typename T>
+__device__ __forceinline__ uint32_t row_load_top(uint32_t addr, pair_t (&v)[4]) {
+  const uint4 r = lds128(addr);
+  if (sizeof(T) == 2) {
+    unpack8(r, v);
+    return ckpt_top(r, T());
+  }
+  const uint4 q = lds128(addr + 16);
+  unpack8(r, q, v);
+  return max(ckpt_top(r, T()), ckpt_top(q, T()));
+}
 
 // A parameter vector in shared memory as two planes of C / 2 floats: the first and the second four of
 // every 8 columns, so that neighbouring lanes read neighbouring 16 bytes.
@@ -146,7 +158,7 @@ struct Place {
     tw = w - team * a.team;
     sub = lane / LANES;
     c0 = (tw * 32 + (lane & (LANES - 1))) * 8;
-    stride = a.team * 256;
+    stride = a.team * LANES * 8;
   }
 };
 
@@ -197,7 +209,7 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) norm_fwd_kernel(NormArgs a)
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int left = a.C - (me.tw * 256 + j * me.stride);
-    mine += left < 0 ? 0 : (left < 256 ? left : 256);
+    mine += left < 0 ? 0 : (left < LANES * 8 ? left : LANES * 8);
   }
   const float inv_c = 1.f / static_cast<float>(a.C), inv_mine = mine ? 1.f / static_cast<float>(mine) : 0.f;
   int slot = 0, s = 0;
@@ -219,11 +231,13 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) norm_fwd_kernel(NormArgs a)
       }
       const uint32_t x_at = smem_u32(st) + (r * a.C + me.c0) * ES;
       pair_t v[NV][4];
+      uint32_t top[NV];
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int c = me.c0 + j * me.stride;
-        if (FULL || (c < a.C && live)) {
-          row_load<T, SRC>(x_at + j * me.stride * ES, SRC ? now.scale[j] : 0.f, v[j]);
+        top[j] = 0;
+        if (FULL || (me.c0 + j * me.stride < a.C && live)) {
+          if (KIND == 1) top[j] = row_load_top<T>(x_at + j * me.stride * ES, v[j]);
+          else row_load<T, SRC>(x_at + j * me.stride * ES, SRC ? now.scale[j] : 0.f, v[j]);
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) v[j][i] = 0;
@@ -278,18 +292,32 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) norm_fwd_kernel(NormArgs a)
         __syncwarp();
         if (leader) norm_fetch<T, SRC, 0>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
       }
+      // Checkpoint scales: the group of vector j lies in GROUP_LANES lanes (a warp holds a group per vector
+      // and GROUP_LANES lanes); lane j of them does its divisions, so that all groups share one round of them.
+      constexpr int GROUP_LANES = LANES < 16 ? LANES : 16;
+      GroupScale held = {};
+      if (KIND == 1) {
+        uint32_t mine_top = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+          for (int o = GROUP_LANES / 2; o > 0; o >>= 1) top[j] = max(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
+          if ((me.lane & (GROUP_LANES - 1)) == j) mine_top = top[j];
+        }
+        held = ckpt_scale_of(mine_top);
+        const int j = me.lane & (GROUP_LANES - 1), c = me.c0 - j * 8 + j * me.stride;
+        if (j < NV && c < a.C && live) a.scales_out[row * a.G + c / CKPT_GROUP] = held.scale;
+      }
       const pair_t rs = both(rstd), off = both(-mean * rstd);
       T* out = static_cast<T*>(a.y) + row * a.C + me.c0;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         const bool in = FULL || (me.c0 + j * me.stride < a.C && live);
         if (KIND == 1) {
-          const GroupScale gs = ckpt_group_scale<(LANES < 16 ? LANES : 16)>(v[j]);
-          if (in) {
-            *reinterpret_cast<uint2*>(a.codes_out + row * a.C + me.c0 + j * me.stride) = ckpt_codes(v[j], gs);
-            if ((me.lane & (LANES < 16 ? LANES - 1 : 15)) == 0)
-              a.scales_out[row * a.G + (me.c0 + j * me.stride) / CKPT_GROUP] = gs.scale;
-          }
+          GroupScale gs;
+          gs.scale = 0.f;
+          gs.factor = __shfl_sync(0xffffffffu, held.factor, (me.lane & ~(GROUP_LANES - 1)) + j);
+          if (in) *reinterpret_cast<uint2*>(a.codes_out + row * a.C + me.c0 + j * me.stride) = ckpt_codes(v[j], gs);
         }
         if (in) {
           pair_t o[4], gm[4], bt[4];
@@ -309,11 +337,13 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) norm_fwd_kernel(NormArgs a)
   if (leader) norm_drain(full, a.stages, requested, ctl);
 }
 
-// Backward.  A lane holds x, dY and gamma of its columns of the row between the sums and dX.  The
-// block writes one partial row of dgamma and dbeta at its end.
+// Backward.  A lane holds xh and g of its columns of the row between the sums and dX; with 16 warps
+// (rows beyond 8192 columns, one team) there are no registers for that, and the row is read from the
+// ring once more.  The block writes one partial row of dgamma and dbeta at its end.
 template <typename T, int NV, int SRC, int FULL, int LANES, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
   constexpr int XS = SRC ? 1 : static_cast<int>(sizeof(T)), DS = sizeof(T), AT_ONCE = 32 / LANES;
+  constexpr bool HOLD = WARPS == BWD_WARPS;
   extern __shared__ __align__(128) uint8_t smem[];
   const Place<WARPS, LANES> me(a);
   float* s_gamma = reinterpret_cast<float*>(smem + me.teams * a.stages * a.stage_bytes);
@@ -354,23 +384,23 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
       const float mean = now.mean, rstd = now.rstd;
       const uint32_t x_at = smem_u32(st) + (r * a.C + me.c0) * XS, d_at = smem_u32(st) + dy_off + (r * a.C + me.c0) * DS;
       const pair_t rs = both(rstd), off = both(-mean * rstd);
-      pair_t x[NV][4], g[NV][4];
+      pair_t xs[HOLD ? NV : 1][4], gs[HOLD ? NV : 1][4];
       pair_t sg[2] = {0, 0}, sx[2] = {0, 0};      // sums of g and g xh
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         if (FULL || (me.c0 + j * me.stride < a.C && live)) {
-          pair_t gm[4];
-          row_load<T, 0>(d_at + j * me.stride * DS, 0.f, g[j]);
-          row_load<T, SRC>(x_at + j * me.stride * XS, now.scale[j], x[j]);
+          pair_t (&x)[4] = xs[HOLD ? j : 0], (&g)[4] = gs[HOLD ? j : 0], gm[4];
+          row_load<T, 0>(d_at + j * me.stride * DS, 0.f, g);
+          row_load<T, SRC>(x_at + j * me.stride * XS, now.scale[j], x);
           planes_load(gamma_at + j * me.stride * 2, plane, gm);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            x[j][i] = fma2(x[j][i], rs, off);
-            dg[j][i] = fma2(g[j][i], x[j][i], dg[j][i]);
-            db[j][i] = add2(db[j][i], g[j][i]);
-            g[j][i] = mul2(g[j][i], gm[i]);
-            sg[i & 1] = add2(sg[i & 1], g[j][i]);
-            sx[i & 1] = fma2(g[j][i], x[j][i], sx[i & 1]);
+            x[i] = fma2(x[i], rs, off);
+            dg[j][i] = fma2(g[i], x[i], dg[j][i]);
+            db[j][i] = add2(db[j][i], g[i]);
+            g[i] = mul2(g[i], gm[i]);
+            sg[i & 1] = add2(sg[i & 1], g[i]);
+            sx[i & 1] = fma2(g[i], x[i], sx[i & 1]);
           }
         }
       }
@@ -387,22 +417,39 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
           sum.y += __shfl_xor_sync(0xffffffffu, sum.y, k);
         }
       }
-      // The item is in registers, of every warp of the team: its stage takes the next one.
-      if (r0 + AT_ONCE >= rows) {
+      // The item has been read by every warp of the team: its stage takes the next one.
+      auto refill = [&]() {
+        if (r0 + AT_ONCE < rows) return;
         __syncwarp();
         if (leader) norm_fetch<T, SRC, 1>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
-      }
+      };
+      if (HOLD) refill();
       // dX = rstd g + xh * (-rstd mean(g xh)) - rstd mean(g)
       const pair_t k1 = both(-rstd * sum.x * inv_c), k2 = both(-rstd * sum.y * inv_c);
       T* out = static_cast<T*>(a.y) + (row0 + r) * a.C + me.c0;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         if (FULL || (me.c0 + j * me.stride < a.C && live)) {
-          pair_t o[4];
+          pair_t (&x)[4] = xs[HOLD ? j : 0], (&g)[4] = gs[HOLD ? j : 0], o[4];
+          if (!HOLD) {
+            pair_t gm[4];
+            row_load<T, 0>(d_at + j * me.stride * DS, 0.f, g);
+            row_load<T, SRC>(x_at + j * me.stride * XS, now.scale[j], x);
+            planes_load(gamma_at + j * me.stride * 2, plane, gm);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = fma2(g[j][i], rs, fma2(x[j][i], k2, k1));
+            for (int i = 0; i < 4; ++i) {
+              x[i] = fma2(x[i], rs, off);
+              g[i] = mul2(g[i], gm[i]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = fma2(g[i], rs, fma2(x[i], k2, k1));
           store8(out + j * me.stride, o);
         }
+      }
+      if (!HOLD) {
+        named_barrier(1 + me.team, a.team * 32);
+        refill();
       }
     }
     if (++s == a.stages) {
@@ -415,12 +462,14 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
   // more), and write the block's part.
   if (LANES < 32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int o = LANES; o < 32; o <<= 1) {
-        dg[0][i] = add2(dg[0][i], __shfl_xor_sync(0xffffffffu, dg[0][i], o));
-        db[0][i] = add2(db[0][i], __shfl_xor_sync(0xffffffffu, db[0][i], o));
-      }
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int o = LANES; o < 32; o <<= 1) {
+          dg[j][i] = add2(dg[j][i], __shfl_xor_sync(0xffffffffu, dg[j][i], o));
+          db[j][i] = add2(db[j][i], __shfl_xor_sync(0xffffffffu, db[j][i], o));
+        }
   }
   float* out = a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.C;
   float* mine = me.teams == 1 ? out : reinterpret_cast<float*>(smem) + me.team * 2 * a.C;
@@ -474,7 +523,9 @@ Shape norm_shape(int64_t M, int64_t C, int sm_count) {
   Shape s;
   const int c = static_cast<int>(C);
   s.warps = !BWD ? FWD_WARPS : C <= 1024 * BWD_WARPS ? BWD_WARPS : WIDE_WARPS;
-  s.lanes = C <= 64 ? 8 : C <= 128 ? 16 : 32;
+  // short rows: 8 or 16 lanes a row.  In the forward 16 lanes have to hold a checkpoint group beyond 64
+  // columns, with or without a checkpoint, so that saving one does not change the order of the sums.
+  s.lanes = C <= (BWD ? 256 : 64) ? 8 : C <= 512 ? 16 : 32;
   s.team = 1;
   while (s.team < s.warps && static_cast<int64_t>(s.team) * 1024 < C) s.team *= 2;
   const int extra = (BWD ? 1 : 2) * c * 4 + static_cast<int>(sizeof(NormCtl));      // gamma (and beta)
@@ -483,8 +534,8 @@ Shape norm_shape(int64_t M, int64_t C, int sm_count) {
   // the ring's share, or two rows of every team where that is more and there is room for it
   const int want = BWD ? BWD_RING : FWD_RING, two = 2 * (s.warps / s.team) * row_bytes;
   if (room > (want > two ? want : two)) room = want > two ? want : two;
-  while (s.team < s.warps && 2 * (s.warps / s.team) * row_bytes > room) s.team *= 2;
-  s.nv = static_cast<int>(ceil_div(C, 256 * s.team));
+  s.nv = static_cast<int>(ceil_div(C, 8 * s.lanes * s.team));
+  if (s.nv == 3 && s.lanes < 32) s.nv = 4;
   const int teams = s.warps / s.team, at_once = 32 / s.lanes;
   // short rows go several to a copy, as long as every team still gets one
   int64_t R = ITEM_BYTES / (c * static_cast<int>(sizeof(T))) > 1 ? ITEM_BYTES / (c * static_cast<int>(sizeof(T))) : 1;
@@ -516,39 +567,25 @@ NormArgs norm_args(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, co
   return a;
 }
 
-// The kernels of a shape.  Rows of up to 128 columns have 8 or 16 lanes to a row and one vector per lane;
-// FULL kernels run where every lane's columns exist; the backward has 8 warps, 16 beyond 8192 columns.
+// The kernels of a shape.  FULL kernels run where every lane's columns exist; the backward has 8 warps, 16
+// beyond 8192 columns.
 typedef void (*NormKernel)(NormArgs);
-template <typename T, int NV, int KIND>
-NormKernel fwd_kernel_nv(bool full) {
-  return full ? norm_fwd_kernel<T, NV, KIND, 1, 32> : norm_fwd_kernel<T, NV, KIND, 0, 32>;
-}
 template <typename T, int KIND>
 NormKernel fwd_kernel(int lanes, int nv, bool full) {
   if (lanes == 8) return norm_fwd_kernel<T, 1, KIND, 0, 8>;
-  if (lanes == 16) return norm_fwd_kernel<T, 1, KIND, 0, 16>;
-  switch (nv) {
-    case 1: return fwd_kernel_nv<T, 1, KIND>(full);
-    case 2: return fwd_kernel_nv<T, 2, KIND>(full);
-    case 3: return fwd_kernel_nv<T, 3, KIND>(full);
-    default: return fwd_kernel_nv<T, 4, KIND>(full);
-  }
-}
-template <typename T, int NV, int SRC, int WARPS>
-NormKernel bwd_kernel_nv(bool full) {
-  return full ? norm_bwd_kernel<T, NV, SRC, 1, 32, WARPS> : norm_bwd_kernel<T, NV, SRC, 0, 32, WARPS>;
+  if (lanes == 16)
+    return nv == 1 ? norm_fwd_kernel<T, 1, KIND, 0, 16> : nv == 2 ? norm_fwd_kernel<T, 2, KIND, 0, 16> : norm_fwd_kernel<T, 4, KIND, 0, 16>;
+  if (nv == 3) return full ? norm_fwd_kernel<T, 3, KIND, 1, 32> : norm_fwd_kernel<T, 3, KIND, 0, 32>;
+  return full ? norm_fwd_kernel<T, 4, KIND, 1, 32> : norm_fwd_kernel<T, 4, KIND, 0, 32>;
 }
 template <typename T, int SRC>
 NormKernel bwd_kernel(int warps, int lanes, int nv, bool full) {
-  if (warps == WIDE_WARPS) return nv == 3 ? bwd_kernel_nv<T, 3, SRC, WIDE_WARPS>(full) : bwd_kernel_nv<T, 4, SRC, WIDE_WARPS>(full);
-  if (lanes == 8) return norm_bwd_kernel<T, 1, SRC, 0, 8, BWD_WARPS>;
-  if (lanes == 16) return norm_bwd_kernel<T, 1, SRC, 0, 16, BWD_WARPS>;
-  switch (nv) {
-    case 1: return bwd_kernel_nv<T, 1, SRC, BWD_WARPS>(full);
-    case 2: return bwd_kernel_nv<T, 2, SRC, BWD_WARPS>(full);
-    case 3: return bwd_kernel_nv<T, 3, SRC, BWD_WARPS>(full);
-    default: return bwd_kernel_nv<T, 4, SRC, BWD_WARPS>(full);
-  }
+  if (warps == WIDE_WARPS) return nv == 3 ? norm_bwd_kernel<T, 3, SRC, 0, 32, WIDE_WARPS> : norm_bwd_kernel<T, 4, SRC, 0, 32, WIDE_WARPS>;
+  if (lanes == 32 && nv == 3) return full ? norm_bwd_kernel<T, 3, SRC, 1, 32, BWD_WARPS> : norm_bwd_kernel<T, 3, SRC, 0, 32, BWD_WARPS>;
+  if (lanes == 32) return full ? norm_bwd_kernel<T, 4, SRC, 1, 32, BWD_WARPS> : norm_bwd_kernel<T, 4, SRC, 0, 32, BWD_WARPS>;
+  if (lanes == 16) return norm_bwd_kernel<T, 4, SRC, 0, 16, BWD_WARPS>;
+  return nv == 1 ? norm_bwd_kernel<T, 1, SRC, 0, 8, BWD_WARPS>
+                 : nv == 2 ? norm_bwd_kernel<T, 2, SRC, 0, 8, BWD_WARPS> : norm_bwd_kernel<T, 4, SRC, 0, 8, BWD_WARPS>;
 }
 
 bool launch_norm(NormKernel k, const NormArgs& a, const Shape& s, cudaStream_t st) {
@@ -564,7 +601,7 @@ int fwd_t(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float
   a.y = y; a.mean = mean; a.rstd = rstd;
   if (out) { a.codes_out = out->codes; a.scales_out = out->scales; }
   count_launches(1);
-  const bool full = C == 256 * s.nv * s.team;
+  const bool full = s.lanes == 32 && C == 256 * s.nv * s.team;
   const bool ok = launch_norm(in    ? fwd_kernel<T, 2>(s.lanes, s.nv, full)
                               : out ? fwd_kernel<T, 1>(s.lanes, s.nv, full)
                                     : fwd_kernel<T, 0>(s.lanes, s.nv, full), a, s, st);
@@ -581,7 +618,7 @@ int bwd_t(const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_
   a.y = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
   a.part = part;
   count_launches(2);
-  const bool full = C == 256 * s.nv * s.team;
+  const bool full = s.lanes == 32 && C == 256 * s.nv * s.team;
   bool ok = launch_norm(in ? bwd_kernel<T, 1>(s.warps, s.lanes, s.nv, full) : bwd_kernel<T, 0>(s.warps, s.lanes, s.nv, full),
                         a, s, st);
   ok = ok && launch_dependent(norm_reduce_kernel, static_cast<unsigned>(ceil_div(2 * C, 32)), 256, 0, st, 1,
@@ -596,14 +633,12 @@ template <typename T>
 bool allow_rings() {
   bool ok = true;
   for (int lanes = 8; lanes <= 32; lanes *= 2)
-    for (int nv = 1; nv <= (lanes == 32 ? 4 : 1); ++nv)
-      for (int full = 0; full < (lanes == 32 ? 2 : 1); ++full) {
+    for (int nv = 1; nv <= 4; ++nv)
+      for (int full = 0; full < 2; ++full)
         ok = ok && big_smem(fwd_kernel<T, 0>(lanes, nv, full)) && big_smem(fwd_kernel<T, 1>(lanes, nv, full)) &&
-             big_smem(fwd_kernel<T, 2>(lanes, nv, full));
-        ok = ok && big_smem(bwd_kernel<T, 0>(BWD_WARPS, lanes, nv, full)) && big_smem(bwd_kernel<T, 1>(BWD_WARPS, lanes, nv, full));
-        if (nv >= 3)
-          ok = ok && big_smem(bwd_kernel<T, 0>(WIDE_WARPS, lanes, nv, full)) && big_smem(bwd_kernel<T, 1>(WIDE_WARPS, lanes, nv, full));
-      }
+             big_smem(fwd_kernel<T, 2>(lanes, nv, full)) && big_smem(bwd_kernel<T, 0>(BWD_WARPS, lanes, nv, full)) &&
+             big_smem(bwd_kernel<T, 1>(BWD_WARPS, lanes, nv, full)) && big_smem(bwd_kernel<T, 0>(WIDE_WARPS, lanes, nv, full)) &&
+             big_smem(bwd_kernel<T, 1>(WIDE_WARPS, lanes, nv, full));
   return ok;
 }
 

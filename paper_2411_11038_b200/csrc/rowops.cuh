@@ -89,20 +89,12 @@ __device__ __forceinline__ void store8(float* p, const pair_t (&v)[4]) {
   reinterpret_cast<ulonglong2*>(p)[1] = make_ulonglong2(v[2], v[3]);
 }
 
-// Scale and multiplier of the group that LANES neighbouring lanes hold (16, or 8 for rows of up to 64
-// columns).  The largest magnitude is taken over the bit patterns, where infinity and NaN rank above
-// every finite value.  Every lane of the warp has to take part.
+// Scale and multiplier of a checkpoint group from the bit pattern of its largest magnitude.  Magnitudes
+// are compared as bit patterns, where infinity and NaN rank above every finite value.
 struct GroupScale {
   float scale, factor;     // value of one code step; multiplier that decides the codes
 };
-template <int LANES = 16>
-__device__ __forceinline__ GroupScale ckpt_group_scale(const pair_t (&v)[4]) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    top = max(top, max(static_cast<uint32_t>(v[i]) & 0x7fffffffu, static_cast<uint32_t>(v[i] >> 32) & 0x7fffffffu));
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+__device__ __forceinline__ GroupScale ckpt_scale_of(uint32_t top) {
   const float a = __uint_as_float(top);
   GroupScale g;
   if (top >= 0x7f800000u) {
@@ -117,18 +109,31 @@ __device__ __forceinline__ GroupScale ckpt_group_scale(const pair_t (&v)[4]) {
   }
   return g;
 }
-
+// Largest magnitude of 16 bytes of elements: 8 bf16 two at a time (the maximum that keeps NaN, on values
+// without their signs), or 4 fp32.
+__device__ __forceinline__ uint32_t ckpt_top(const uint4& r, bf16) {
+  auto h = [](uint32_t w) {
+    w &= 0x7fff7fffu;
+    return *reinterpret_cast<const __nv_bfloat162*>(&w);
+  };
+  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h(r.x), h(r.y)), __hmax2_nan(h(r.z), h(r.w)));
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(&m);
+  return max(w << 16, w & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t ckpt_top(const uint4& r, float) {
+  return max(max(r.x & 0x7fffffffu, r.y & 0x7fffffffu), max(r.z & 0x7fffffffu, r.w & 0x7fffffffu));
+}
 // The 8 codes of a lane as two words.  Adding 1.5 * 2^23 rounds to nearest-even and leaves the code
 // in the low byte of the sum's bit pattern (two's complement), so no conversion instruction is used.
 __device__ __forceinline__ uint2 ckpt_codes(const pair_t (&v)[4], const GroupScale& g) {
   uint32_t c[8];
-  const pair_t f = both(g.factor);
+  const pair_t f = both(g.factor), one = both(1.f), magic = both(12582912.f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    // the product is rounded before the sum (one by one: a packed product and sum came out fused)
-    const float2 q = halves(mul2(v[i], f));
-    c[2 * i] = __float_as_uint(__fadd_rn(q.x, 12582912.f));
-    c[2 * i + 1] = __float_as_uint(__fadd_rn(q.y, 12582912.f));
+    // the product is rounded before the sum: a packed product and a packed sum came out fused
+    const float2 q = halves(fma2(mul2(v[i], f), one, magic));
+    c[2 * i] = __float_as_uint(q.x);
+    c[2 * i + 1] = __float_as_uint(q.y);
   }
   uint2 w;
   w.x = __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
