@@ -71,28 +71,6 @@ struct RowArgs {
   int wide;                 // x, dy and y are 32-byte aligned
 };
 
-// 32 bytes of 16 (bf16) or 8 (fp32) elements.
-__device__ __forceinline__ void load32(const void* p, int wide, uint4& a, uint4& b) {
-  if (wide) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
-                 : "l"(p));
-  } else {
-    a = reinterpret_cast<const uint4*>(p)[0];
-    b = reinterpret_cast<const uint4*>(p)[1];
-  }
-}
-__device__ __forceinline__ void store32(void* p, int wide, const uint4& a, const uint4& b) {
-  if (wide) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z),
-                 "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
-                 : "memory");
-  } else {
-    reinterpret_cast<uint4*>(p)[0] = a;
-    reinterpret_cast<uint4*>(p)[1] = b;
-  }
-}
-
 // 16 consecutive elements of a lane.
 template <typename T>
 struct Vec16;

@@ -5,12 +5,17 @@
 //   g  = dY gamma,  xh = (x - mean) rstd,  dX = rstd (g - mean_c(g) - xh mean_c(g xh))
 //   dgamma = sum_m dY xh,  dbeta = sum_m dY
 //
-// HBM-bound: every tensor is touched once.  Persistent blocks, one per SM, whose warps form teams of
-// 1, 2, 4, 8 or 16: a team takes a row, a lane up to 32 of its columns (8, 16 or 32 lanes and one
-// warp where rows are short), the same columns in every row, so that the running dgamma and dbeta
-// stay in registers.  Each team keeps a ring of its next rows in shared memory, filled by bulk copies
-// that it requests itself as soon as it has read a row; teams of one warp (up to 1024 columns) never
-// wait for each other.
+// HBM-bound: every tensor is touched once.  A row belongs to a team of 1, 2, 4, 8 or 16 warps, a lane to up
+// to 32 of its columns (8 or 16 lanes and one warp where rows are short).
+//
+// Forward: the simplest form at the highest occupancy, one row per team and no loop.  (A persistent
+// form with rows prefetched into shared memory was measured too: 16 warps with their row's chain of
+// reductions do not cover an SM's share of the bandwidth; 16384 x 4096 bf16 47.6 us.)
+//
+// Backward: persistent blocks, one per SM, since dgamma and dbeta want each lane to keep its columns: their
+// running sums stay in registers over all rows of the team.  Each team keeps a ring of its next rows
+// in shared memory, filled by bulk copies that it requests itself as soon as it has read a row;
+// teams of one warp (up to 1024 columns) never wait for each other.
 //
 // A warp forms the variance around the mean of its own columns, and the warps' parts are joined
 // exactly (M2 = sum M2_w + sum n_w (mean_w - mean)^2): no cancellation for rows far from zero, one
@@ -27,10 +32,10 @@ namespace {
 static const int RING_MAX = 8;
 static const int WHOLE_BLOCK = 15;            // barrier id; teams of several warps use 1 + team (at most 8)
 static const int ITEM_BYTES = 2048;           // short rows: as many to a copy as make up about this
-// Warps of a block and bytes of its ring: the forward hides its row's chain of reductions behind other
-// rows, the backward wants the registers of few warps (it holds a row's x and dY and its 64 sums).
-static const int FWD_WARPS = 16, BWD_WARPS = 8, WIDE_WARPS = 16;
-static const int FWD_RING = 64 * 1024, BWD_RING = 112 * 1024;
+// Warps of a backward block and bytes of its ring: few warps with many registers (a lane holds a row's xh
+// and g and its 64 sums); beyond 8192 columns one team of 16.
+static const int BWD_WARPS = 8, WIDE_WARPS = 16;
+static const int BWD_RING = 112 * 1024;
 
 struct NormArgs {
   const void* x; const int8_t* codes_in; const float* scales_in;
@@ -41,6 +46,7 @@ struct NormArgs {
   int64_t M;
   int C, G, team;                                         // columns, checkpoint groups per row, warps per row
   int R, stages, stage_bytes, items;                      // rows per item (copy), stages per team
+  int wide;                                               // gamma and beta are 32-byte aligned
   int* status;
 };
 
@@ -50,10 +56,10 @@ struct __align__(16) NormCtl {
   int abort_flag;
 };
 
-// Bytes of an item of R rows in the ring: x (or its codes), then (backward) dY.
-template <typename T, int SRC, int BWD>
+// Bytes of an item of R rows in the ring: x (or its codes), then dY.
+template <typename T, int SRC>
 __host__ __device__ __forceinline__ int item_bytes(int R, int C) {
-  return (R * C * ((SRC ? 1 : static_cast<int>(sizeof(T))) + (BWD ? static_cast<int>(sizeof(T)) : 0)) + 127) & ~127;
+  return (R * C * (SRC ? 1 + static_cast<int>(sizeof(T)) : 2 * static_cast<int>(sizeof(T))) + 127) & ~127;
 }
 
 // Waits unless something has already run out; a wait that runs out is reported and the block goes on
@@ -71,7 +77,7 @@ __device__ __forceinline__ void norm_wait(uint64_t* bar, uint32_t parity, NormCt
 // One thread: requests an item into a stage of its team's ring (nothing past the last item, or after a
 // wait ran out).  The team has read what the stage held; the proxy fence orders those reads before
 // the copy's writes.
-template <typename T, int SRC, int BWD>
+template <typename T, int SRC>
 __device__ __forceinline__ void norm_fetch(const NormArgs& a, int64_t item, uint8_t* st, uint64_t* bar, NormCtl* ctl,
                                            int& requested) {
   if (item >= a.items || *static_cast<volatile int*>(&ctl->abort_flag)) return;
@@ -79,12 +85,12 @@ __device__ __forceinline__ void norm_fetch(const NormArgs& a, int64_t item, uint
   const int64_t row0 = item * a.R;
   const int rows = a.M - row0 < a.R ? static_cast<int>(a.M - row0) : a.R;
   const uint32_t n = static_cast<uint32_t>(rows) * a.C;
-  const uint32_t xb = n * (SRC ? 1u : static_cast<uint32_t>(sizeof(T))), db = BWD ? n * static_cast<uint32_t>(sizeof(T)) : 0u;
+  const uint32_t xb = n * (SRC ? 1u : static_cast<uint32_t>(sizeof(T))), db = n * static_cast<uint32_t>(sizeof(T));
   fence_proxy_async();
   mbar_arrive_expect_tx(bar, xb + db);
   if (SRC) bulk_load(st, a.codes_in + row0 * a.C, xb, bar);
   else bulk_load(st, static_cast<const T*>(a.x) + row0 * a.C, xb, bar);
-  if (BWD) bulk_load(st + a.R * a.C * (SRC ? 1 : static_cast<int>(sizeof(T))), static_cast<const T*>(a.dy) + row0 * a.C, db, bar);
+  bulk_load(st + a.R * a.C * (SRC ? 1 : static_cast<int>(sizeof(T))), static_cast<const T*>(a.dy) + row0 * a.C, db, bar);
 }
 
 // After a wait ran out: none of the team's copies may be in flight when the block exits.
@@ -109,18 +115,6 @@ __device__ __forceinline__ void row_load(uint32_t addr, float scale, pair_t (&v)
   if (SRC) ckpt_values(lds64(addr), scale, v);
   else if (sizeof(T) == 2) unpack8(lds128(addr), v);
   else unpack8(lds128(addr), lds128(addr + 16), v);
-}
-// ... and their largest magnitude.
-template <typename T>
-__device__ __forceinline__ uint32_t row_load_top(uint32_t addr, pair_t (&v)[4]) {
-  const uint4 r = lds128(addr);
-  if (sizeof(T) == 2) {
-    unpack8(r, v);
-    return ckpt_top(r, T());
-  }
-  const uint4 q = lds128(addr + 16);
-  unpack8(r, q, v);
-  return max(ckpt_top(r, T()), ckpt_top(q, T()));
 }
 
 // A parameter vector in shared memory as two planes of C / 2 floats: the first and the second four of
@@ -182,159 +176,163 @@ struct RowStats {
   }
 };
 
-// KIND 0: y, mean, rstd; 1: and the checkpoint of x; 2: y from a checkpoint and the given statistics.
-// FULL: every lane's NV vectors lie within the row (C = 256 NV team).
-template <typename T, int NV, int KIND, int FULL, int LANES>
-__global__ void __launch_bounds__(32 * FWD_WARPS, 1) norm_fwd_kernel(NormArgs a) {
-  constexpr int SRC = KIND == 2, ES = SRC ? 1 : static_cast<int>(sizeof(T)), AT_ONCE = 32 / LANES;
-  extern __shared__ __align__(128) uint8_t smem[];
-  const Place<FWD_WARPS, LANES> me(a);
-  float* s_gamma = reinterpret_cast<float*>(smem + me.teams * a.stages * a.stage_bytes);
-  NormCtl* ctl = norm_setup(a, me.teams, reinterpret_cast<uint8_t*>(s_gamma + 2 * a.C));
-  uint8_t* ring = smem + me.team * a.stages * a.stage_bytes;
-  uint64_t* full = ctl->full + me.team * a.stages;
-  const int first = blockIdx.x * me.teams + me.team, step = gridDim.x * me.teams;
-  const bool leader = me.tw == 0 && me.lane == 0;
-  int requested = 0;
+// Raw elements of a lane: kept as they are in memory between the passes over the row (a bf16 row takes
+// half the registers of its values), which is what lets 40 and more warps share an SM.
+template <typename T, int SRC>
+struct Raw {
+  uint4 r[SRC ? 1 : sizeof(T) / 2];
+  __device__ __forceinline__ void zero() {
+    r[0] = make_uint4(0, 0, 0, 0);
+    if (!SRC && sizeof(T) == 4) r[sizeof(r) / 16 - 1] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void load(const void* x, const int8_t* codes, int64_t at) {
+    if (SRC) {
+      const uint2 w = *reinterpret_cast<const uint2*>(codes + at);
+      r[0].x = w.x;
+      r[0].y = w.y;
+    } else {
+      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(x) + at);
+      r[0] = p[0];
+      if (sizeof(T) == 4) r[sizeof(r) / 16 - 1] = p[1];
+    }
+  }
+  __device__ __forceinline__ void get(float scale, pair_t (&v)[4]) const {
+    if (SRC) ckpt_values(make_uint2(r[0].x, r[0].y), scale, v);
+    else if (sizeof(T) == 2) unpack8(r[0], v);
+    else unpack8(r[0], r[sizeof(r) / 16 - 1], v);
+  }
+  // From here on the elements are unpacked anew: their unpacked values are not worth registers.
+  __device__ __forceinline__ void forget() {
+    if (sizeof(T) == 2) asm volatile("" : "+r"(r[0].x), "+r"(r[0].y), "+r"(r[0].z), "+r"(r[0].w));
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    return max(ckpt_top(r[0], T()), ckpt_top(r[sizeof(r) / 16 - 1], T()));
+  }
+};
+
+// Forward.  KIND 0: y, mean, rstd; 1: and the checkpoint of x; 2: y from a checkpoint and the given
+// statistics.  One row per team; blocks of one team, or of 4 warps where a warp holds one or several
+// rows.  gamma and beta come through L1, where a block's predecessors on the SM have left them.
+template <typename T, int NV, int KIND, int LANES>
+__global__ void __maxnreg__(sizeof(T) == 4 ? 64 : NV > 2 ? 48 : 40) norm_fwd_kernel(NormArgs a) {
+  constexpr int SRC = KIND == 2, AT_ONCE = 32 / LANES;
+  __shared__ float4 s_red[16];
   pdl_trigger();
   pdl_wait();
-  if (leader)
-    for (int s = 0; s < a.stages; ++s)
-      norm_fetch<T, SRC, 0>(a, static_cast<int64_t>(first) + s * step, ring + s * a.stage_bytes, &full[s], ctl, requested);
-  planes_fill(s_gamma, a.gamma, a.C);
-  planes_fill(s_gamma + a.C, a.beta, a.C);
-  __syncthreads();
-  const uint32_t gamma_at = smem_u32(s_gamma) + me.c0 * 2, beta_at = gamma_at + a.C * 4, plane = a.C * 2;
-  int mine = 0;                       // this warp's columns
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int tw = a.team == 1 ? 0 : w, c0 = (tw * 32 + (lane & (LANES - 1))) * 8, stride = a.team * LANES * 8;
+  const int64_t row = a.team == 1 ? (static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + w) * AT_ONCE + lane / LANES : blockIdx.x;
+  const bool live = row < a.M;
+  const int64_t base = row * a.C + c0;
+  Raw<T, SRC> x[NV];
+  float scale[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int left = a.C - (me.tw * 256 + j * me.stride);
-    mine += left < 0 ? 0 : (left < LANES * 8 ? left : LANES * 8);
+    x[j].zero();
+    scale[j] = 0.f;
+    if (live && c0 + j * stride < a.C) {
+      x[j].load(a.x, a.codes_in, base + j * stride);
+      if (SRC) scale[j] = a.scales_in[row * a.G + (c0 + j * stride) / CKPT_GROUP];
+    }
   }
-  const float inv_c = 1.f / static_cast<float>(a.C), inv_mine = mine ? 1.f / static_cast<float>(mine) : 0.f;
-  int slot = 0, s = 0;
-  uint32_t ph = 0;
-  RowStats<NV, SRC> next = {}, now;
-  if (SRC) next.ask(a, static_cast<int64_t>(first) * a.R + me.sub, me.c0, me.stride);
-  for (int64_t item = first; item < a.items; item += step) {
-    const int64_t row0 = item * a.R;
-    const int rows = a.M - row0 < a.R ? static_cast<int>(a.M - row0) : a.R;
-    uint8_t* st = ring + s * a.stage_bytes;
-    norm_wait(&full[s], ph, ctl, a.status);
-    for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
-      const int r = r0 + me.sub;
-      const bool live = AT_ONCE == 1 || r < rows;
-      const int64_t row = row0 + r;
-      if (SRC) {
-        now = next;
-        next.ask(a, (r0 + AT_ONCE < rows ? row + AT_ONCE : (item + step) * a.R + me.sub), me.c0, me.stride);
-      }
-      const uint32_t x_at = smem_u32(st) + (r * a.C + me.c0) * ES;
-      pair_t v[NV][4];
-      uint32_t top[NV];
+  float mean = 0.f, rstd = 0.f;
+  if (SRC == 0) {
+    int mine = 0;                       // this warp's columns
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        top[j] = 0;
-        if (FULL || (me.c0 + j * me.stride < a.C && live)) {
-          if (KIND == 1) top[j] = row_load_top<T>(x_at + j * me.stride * ES, v[j]);
-          else row_load<T, SRC>(x_at + j * me.stride * ES, SRC ? now.scale[j] : 0.f, v[j]);
-        } else {
+    for (int j = 0; j < NV; ++j) {
+      const int left = a.C - (tw * 256 + j * stride);
+      mine += left < 0 ? 0 : (left < LANES * 8 ? left : LANES * 8);
+    }
+    pair_t t[2] = {0, 0};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[j][i] = 0;
-        }
-      }
-      float mean, rstd;
-      if (SRC == 0) {
-        pair_t t[2] = {0, 0};
+    for (int j = 0; j < NV; ++j) {
+      pair_t v[4];
+      x[j].get(0.f, v);
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+      for (int i = 0; i < 4; ++i) t[i & 1] = add2(t[i & 1], v[i]);
+    }
+    mean = mine ? lanes_sum<LANES>(pair_sum(add2(t[0], t[1]))) / static_cast<float>(mine) : 0.f;
+    t[0] = t[1] = 0;
+    const pair_t off = both(-mean);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) t[i & 1] = add2(t[i & 1], v[j][i]);
-        mean = lanes_sum<LANES>(pair_sum(add2(t[0], t[1]))) * inv_mine;
-        t[0] = t[1] = 0;
-        const pair_t off = both(-mean);
+    for (int j = 0; j < NV; ++j) {
+      if (c0 + j * stride < a.C) {
+        pair_t v[4];
+        x[j].forget();
+        x[j].get(0.f, v);
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          if (FULL || me.c0 + j * me.stride < a.C) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const pair_t d = add2(v[j][i], off);
-              t[i & 1] = fma2(d, d, t[i & 1]);
-            }
-          }
-        }
-        float m2 = lanes_sum<LANES>(pair_sum(add2(t[0], t[1])));
-        if (a.team > 1) {
-          float4* red = ctl->red[slot] + me.team * a.team;
-          slot ^= 1;
-          if (me.lane == 0) red[me.tw] = make_float4(mean, m2, static_cast<float>(mine), 0.f);
-          named_barrier(1 + me.team, a.team * 32);
-          const float4 o = red[me.lane & (a.team - 1)];
-          mean = o.z * o.x;
-          for (int k = 1; k < a.team; k <<= 1) mean += __shfl_xor_sync(0xffffffffu, mean, k);
-          mean *= inv_c;
-          m2 = fmaf(o.z * (o.x - mean), o.x - mean, o.y);
-          for (int k = 1; k < a.team; k <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, k);
-        }
-        rstd = rsqrtf(fmaf(m2, inv_c, a.eps));
-        if (me.tw == 0 && (me.lane & (LANES - 1)) == 0 && live) {
-          a.mean[row] = mean;
-          a.rstd[row] = rstd;
-        }
-      } else {
-        mean = now.mean;
-        rstd = now.rstd;
-        if (a.team > 1 && r0 + AT_ONCE >= rows) named_barrier(1 + me.team, a.team * 32);
-      }
-      // The item is in registers, of every warp of the team: its stage takes the team's item after the
-      // ones already requested.
-      if (r0 + AT_ONCE >= rows) {
-        __syncwarp();
-        if (leader) norm_fetch<T, SRC, 0>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
-      }
-      // Checkpoint scales: the group of vector j lies in GROUP_LANES lanes (a warp holds a group per vector
-      // and GROUP_LANES lanes); lane j of them does its divisions, so that all groups share one round of them.
-      constexpr int GROUP_LANES = LANES < 16 ? LANES : 16;
-      GroupScale held = {};
-      if (KIND == 1) {
-        uint32_t mine_top = 0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-#pragma unroll
-          for (int o = GROUP_LANES / 2; o > 0; o >>= 1) top[j] = max(top[j], __shfl_xor_sync(0xffffffffu, top[j], o));
-          if ((me.lane & (GROUP_LANES - 1)) == j) mine_top = top[j];
-        }
-        held = ckpt_scale_of(mine_top);
-        const int j = me.lane & (GROUP_LANES - 1), c = me.c0 - j * 8 + j * me.stride;
-        if (j < NV && c < a.C && live) a.scales_out[row * a.G + c / CKPT_GROUP] = held.scale;
-      }
-      const pair_t rs = both(rstd), off = both(-mean * rstd);
-      T* out = static_cast<T*>(a.y) + row * a.C + me.c0;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const bool in = FULL || (me.c0 + j * me.stride < a.C && live);
-        if (KIND == 1) {
-          GroupScale gs;
-          gs.scale = 0.f;
-          gs.factor = __shfl_sync(0xffffffffu, held.factor, (me.lane & ~(GROUP_LANES - 1)) + j);
-          if (in) *reinterpret_cast<uint2*>(a.codes_out + row * a.C + me.c0 + j * me.stride) = ckpt_codes(v[j], gs);
-        }
-        if (in) {
-          pair_t o[4], gm[4], bt[4];
-          planes_load(gamma_at + j * me.stride * 2, plane, gm);
-          planes_load(beta_at + j * me.stride * 2, plane, bt);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = fma2(fma2(v[j][i], rs, off), gm[i], bt[i]);
-          store8(out + j * me.stride, o);
+        for (int i = 0; i < 4; ++i) {
+          const pair_t d = add2(v[i], off);
+          t[i & 1] = fma2(d, d, t[i & 1]);
         }
       }
     }
-    if (++s == a.stages) {
-      s = 0;
-      ph ^= 1;
+    float m2 = lanes_sum<LANES>(pair_sum(add2(t[0], t[1])));
+    const float inv_c = 1.f / static_cast<float>(a.C);
+    if (a.team > 1) {
+      if (lane == 0) s_red[tw] = make_float4(mean, m2, static_cast<float>(mine), 0.f);
+      __syncthreads();
+      const float4 o = s_red[lane & (a.team - 1)];
+      mean = o.z * o.x;
+      for (int k = 1; k < a.team; k <<= 1) mean += __shfl_xor_sync(0xffffffffu, mean, k);
+      mean *= inv_c;
+      m2 = fmaf(o.z * (o.x - mean), o.x - mean, o.y);
+      for (int k = 1; k < a.team; k <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, k);
+    }
+    rstd = rsqrtf(fmaf(m2, inv_c, a.eps));
+    if (tw == 0 && (lane & (LANES - 1)) == 0 && live) {
+      a.mean[row] = mean;
+      a.rstd[row] = rstd;
+    }
+  } else if (live) {
+    mean = a.mean[row];
+    rstd = a.rstd[row];
+  }
+  // Checkpoint scales: the group of vector j lies in GROUP_LANES lanes (a warp holds a group per vector and
+  // GROUP_LANES lanes); lane j of them does its divisions, so that all groups share one round of them.
+  constexpr int GROUP_LANES = LANES < 16 ? LANES : 16;
+  GroupScale held = {};
+  if (KIND == 1) {
+    uint32_t mine_top = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      uint32_t top = x[j].top();
+#pragma unroll
+      for (int o = GROUP_LANES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if ((lane & (GROUP_LANES - 1)) == j) mine_top = top;
+    }
+    held = ckpt_scale_of(mine_top);
+    const int j = lane & (GROUP_LANES - 1), c = c0 - j * 8 + j * stride;
+    if (j < NV && c < a.C && live) a.scales_out[row * a.G + c / CKPT_GROUP] = held.scale;
+  }
+  const pair_t rs = both(rstd), off = both(-mean * rstd);
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = c0 + j * stride;
+    const bool in = live && c < a.C;
+    pair_t v[4];
+    x[j].forget();
+    x[j].get(scale[j], v);
+    if (KIND == 1) {
+      GroupScale gs;
+      gs.scale = 0.f;
+      gs.factor = __shfl_sync(0xffffffffu, held.factor, (lane & ~(GROUP_LANES - 1)) + j);
+      if (in) *reinterpret_cast<uint2*>(a.codes_out + base + j * stride) = ckpt_codes(v, gs);
+    }
+    if (in) {
+      pair_t gm[4], bt[4] = {0, 0, 0, 0};
+      uint4 lo, hi;
+      load32(a.gamma + c, a.wide, lo, hi);
+      unpack8(lo, hi, gm);
+      if (a.beta) {
+        load32(a.beta + c, a.wide, lo, hi);
+        unpack8(lo, hi, bt);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = fma2(fma2(v[i], rs, off), gm[i], bt[i]);
+      store8(static_cast<T*>(a.y) + base + j * stride, v);
     }
   }
-  if (leader) norm_drain(full, a.stages, requested, ctl);
 }
 
 // Backward.  A lane holds xh and g of its columns of the row between the sums and dX; with 16 warps
@@ -357,7 +355,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
   pdl_wait();
   if (leader)
     for (int s = 0; s < a.stages; ++s)
-      norm_fetch<T, SRC, 1>(a, static_cast<int64_t>(first) + s * step, ring + s * a.stage_bytes, &full[s], ctl, requested);
+      norm_fetch<T, SRC>(a, static_cast<int64_t>(first) + s * step, ring + s * a.stage_bytes, &full[s], ctl, requested);
   planes_fill(s_gamma, a.gamma, a.C);
   __syncthreads();
   const uint32_t gamma_at = smem_u32(s_gamma) + me.c0 * 2, plane = a.C * 2, dy_off = a.R * a.C * XS;
@@ -421,7 +419,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
       auto refill = [&]() {
         if (r0 + AT_ONCE < rows) return;
         __syncwarp();
-        if (leader) norm_fetch<T, SRC, 1>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
+        if (leader) norm_fetch<T, SRC>(a, item + static_cast<int64_t>(a.stages) * step, st, &full[s], ctl, requested);
       };
       if (HOLD) refill();
       // dX = rstd g + xh * (-rstd mean(g xh)) - rstd mean(g)
@@ -512,28 +510,26 @@ __global__ void __launch_bounds__(256) norm_reduce_kernel(const float* __restric
   }
 }
 
-// Shape of a launch: lanes and warps per row (a power of two, so that teams fill the block), vectors per
-// lane, rows per item, ring.
+// Shape of a backward launch: lanes and warps per row (a power of two, so that teams fill the block),
+// vectors per lane, rows per item, ring.
 struct Shape {
   int warps, team, lanes, nv, R, stages, stage_bytes, items, grid;
   size_t smem;
 };
-template <typename T, int SRC, int BWD>
-Shape norm_shape(int64_t M, int64_t C, int sm_count) {
+template <typename T, int SRC>
+Shape bwd_shape(int64_t M, int64_t C, int sm_count) {
   Shape s;
   const int c = static_cast<int>(C);
-  s.warps = !BWD ? FWD_WARPS : C <= 1024 * BWD_WARPS ? BWD_WARPS : WIDE_WARPS;
-  // short rows: 8 or 16 lanes a row.  In the forward 16 lanes have to hold a checkpoint group beyond 64
-  // columns, with or without a checkpoint, so that saving one does not change the order of the sums.
-  s.lanes = C <= (BWD ? 256 : 64) ? 8 : C <= 512 ? 16 : 32;
+  s.warps = C <= 1024 * BWD_WARPS ? BWD_WARPS : WIDE_WARPS;
+  s.lanes = C <= 256 ? 8 : C <= 512 ? 16 : 32;
   s.team = 1;
   while (s.team < s.warps && static_cast<int64_t>(s.team) * 1024 < C) s.team *= 2;
-  const int extra = (BWD ? 1 : 2) * c * 4 + static_cast<int>(sizeof(NormCtl));      // gamma (and beta)
-  const int row_bytes = item_bytes<T, SRC, BWD>(1, c);
+  const int extra = c * 4 + static_cast<int>(sizeof(NormCtl));      // gamma
+  const int row_bytes = item_bytes<T, SRC>(1, c);
   int room = 227 * 1024 - extra;
   // the ring's share, or two rows of every team where that is more and there is room for it
-  const int want = BWD ? BWD_RING : FWD_RING, two = 2 * (s.warps / s.team) * row_bytes;
-  if (room > (want > two ? want : two)) room = want > two ? want : two;
+  const int two = 2 * (s.warps / s.team) * row_bytes;
+  if (room > (BWD_RING > two ? BWD_RING : two)) room = BWD_RING > two ? BWD_RING : two;
   s.nv = static_cast<int>(ceil_div(C, 8 * s.lanes * s.team));
   if (s.nv == 3 && s.lanes < 32) s.nv = 4;
   const int teams = s.warps / s.team, at_once = 32 / s.lanes;
@@ -542,42 +538,38 @@ Shape norm_shape(int64_t M, int64_t C, int sm_count) {
   const int64_t even = ceil_div(M, static_cast<int64_t>(sm_count) * teams);
   if (R > even) R = even;
   s.R = static_cast<int>(round_up(R, at_once));
-  s.stage_bytes = item_bytes<T, SRC, BWD>(s.R, c);
+  s.stage_bytes = item_bytes<T, SRC>(s.R, c);
   s.stages = room / (teams * s.stage_bytes);
   if (s.stages > RING_MAX) s.stages = RING_MAX;
   s.items = static_cast<int>(ceil_div(M, s.R));
   const int64_t blocks = ceil_div(s.items, teams);
   s.grid = static_cast<int>(blocks < sm_count ? blocks : sm_count);
   s.smem = static_cast<size_t>(teams) * s.stages * s.stage_bytes + extra;
-  // the backward joins its teams in the ring: [teams][2][C] floats
-  const size_t join = BWD && teams > 1 ? static_cast<size_t>(teams) * 2 * C * 4 : 0;
+  // the teams are joined in the ring: [teams][2][C] floats
+  const size_t join = teams > 1 ? static_cast<size_t>(teams) * 2 * C * 4 : 0;
   if (s.smem < join) s.smem = join;
   return s;
 }
 
-NormArgs norm_args(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const Shape& s, int* status) {
+NormArgs norm_args(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, int* status) {
   NormArgs a = {};
   a.x = x;
   if (in) { a.codes_in = in->codes; a.scales_in = in->scales; }
   a.M = M;
   a.C = static_cast<int>(C);
   a.G = static_cast<int>(ckpt_groups(C));
-  a.team = s.team; a.R = s.R; a.stages = s.stages; a.stage_bytes = s.stage_bytes; a.items = s.items;
   a.status = status;
   return a;
 }
 
-// The kernels of a shape.  FULL kernels run where every lane's columns exist; the backward has 8 warps, 16
-// beyond 8192 columns.
 typedef void (*NormKernel)(NormArgs);
 template <typename T, int KIND>
-NormKernel fwd_kernel(int lanes, int nv, bool full) {
-  if (lanes == 8) return norm_fwd_kernel<T, 1, KIND, 0, 8>;
-  if (lanes == 16)
-    return nv == 1 ? norm_fwd_kernel<T, 1, KIND, 0, 16> : nv == 2 ? norm_fwd_kernel<T, 2, KIND, 0, 16> : norm_fwd_kernel<T, 4, KIND, 0, 16>;
-  if (nv == 3) return full ? norm_fwd_kernel<T, 3, KIND, 1, 32> : norm_fwd_kernel<T, 3, KIND, 0, 32>;
-  return full ? norm_fwd_kernel<T, 4, KIND, 1, 32> : norm_fwd_kernel<T, 4, KIND, 0, 32>;
+NormKernel fwd_kernel(int lanes, int nv) {
+  if (lanes == 8) return norm_fwd_kernel<T, 1, KIND, 8>;
+  if (lanes == 16) return nv == 1 ? norm_fwd_kernel<T, 1, KIND, 16> : nv == 2 ? norm_fwd_kernel<T, 2, KIND, 16> : norm_fwd_kernel<T, 4, KIND, 16>;
+  return nv == 3 ? norm_fwd_kernel<T, 3, KIND, 32> : norm_fwd_kernel<T, 4, KIND, 32>;
 }
+// FULL kernels run where every lane's columns exist; 8 warps, 16 beyond 8192 columns.
 template <typename T, int SRC>
 NormKernel bwd_kernel(int warps, int lanes, int nv, bool full) {
   if (warps == WIDE_WARPS) return nv == 3 ? norm_bwd_kernel<T, 3, SRC, 0, 32, WIDE_WARPS> : norm_bwd_kernel<T, 4, SRC, 0, 32, WIDE_WARPS>;
@@ -588,39 +580,44 @@ NormKernel bwd_kernel(int warps, int lanes, int nv, bool full) {
                  : nv == 2 ? norm_bwd_kernel<T, 2, SRC, 0, 8, BWD_WARPS> : norm_bwd_kernel<T, 4, SRC, 0, 8, BWD_WARPS>;
 }
 
-bool launch_norm(NormKernel k, const NormArgs& a, const Shape& s, cudaStream_t st) {
-  return launch_dependent(k, static_cast<unsigned>(s.grid), 32u * s.warps, s.smem, st, 1, a) == cudaSuccess;
-}
-
+// 8 or 16 lanes a row where rows are short; 16 lanes have to hold a checkpoint group beyond 64 columns, with
+// or without a checkpoint, so that saving one does not change the order of the sums.
 template <typename T>
 int fwd_t(const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma, const float* beta, float eps,
           void* y, float* mean, float* rstd, const efqat_ckpt* out, int* status, int sm_count, cudaStream_t st) {
-  const Shape s = in ? norm_shape<T, 1, 0>(M, C, sm_count) : norm_shape<T, 0, 0>(M, C, sm_count);
-  NormArgs a = norm_args(x, in, M, C, s, status);
+  NormArgs a = norm_args(x, in, M, C, status);
   a.gamma = gamma; a.beta = beta; a.eps = eps;
+  a.wide = ((reinterpret_cast<uintptr_t>(gamma) | reinterpret_cast<uintptr_t>(beta)) & 31) == 0;
   a.y = y; a.mean = mean; a.rstd = rstd;
   if (out) { a.codes_out = out->codes; a.scales_out = out->scales; }
+  const int lanes = C <= 64 ? 8 : C <= 512 ? 16 : 32;
+  a.team = 1;
+  while (a.team * 1024ll < C) a.team *= 2;
+  int nv = static_cast<int>(ceil_div(C, 8 * lanes * a.team));
+  if (nv == 3 && lanes < 32) nv = 4;
+  // blocks of 4 warps, of fewer where the rows would not reach every SM
+  const int64_t row_warps = ceil_div(M, 32 / lanes);
+  const int warps = a.team > 1 ? a.team : row_warps < 2 * sm_count ? 1 : 4;
+  const int64_t grid = a.team > 1 ? M : ceil_div(row_warps, warps);
+  const NormKernel k = in ? fwd_kernel<T, 2>(lanes, nv) : out ? fwd_kernel<T, 1>(lanes, nv) : fwd_kernel<T, 0>(lanes, nv);
   count_launches(1);
-  const bool full = s.lanes == 32 && C == 256 * s.nv * s.team;
-  const bool ok = launch_norm(in    ? fwd_kernel<T, 2>(s.lanes, s.nv, full)
-                              : out ? fwd_kernel<T, 1>(s.lanes, s.nv, full)
-                                    : fwd_kernel<T, 0>(s.lanes, s.nv, full), a, s, st);
-  return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
+  return launch_dependent(k, static_cast<unsigned>(grid), 32u * warps, 0, st, 1, a) == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
 
 template <typename T>
 int bwd_t(const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_t C, const float* gamma,
           const float* mean, const float* rstd, void* dx, float* dgamma, float* dbeta, float* part, int* status,
           int sm_count, cudaStream_t st) {
-  const Shape s = in ? norm_shape<T, 1, 1>(M, C, sm_count) : norm_shape<T, 0, 1>(M, C, sm_count);
-  NormArgs a = norm_args(x, in, M, C, s, status);
+  const Shape s = in ? bwd_shape<T, 1>(M, C, sm_count) : bwd_shape<T, 0>(M, C, sm_count);
+  NormArgs a = norm_args(x, in, M, C, status);
+  a.team = s.team; a.R = s.R; a.stages = s.stages; a.stage_bytes = s.stage_bytes; a.items = s.items;
   a.dy = dy; a.gamma = gamma;
   a.y = dx; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
   a.part = part;
   count_launches(2);
   const bool full = s.lanes == 32 && C == 256 * s.nv * s.team;
-  bool ok = launch_norm(in ? bwd_kernel<T, 1>(s.warps, s.lanes, s.nv, full) : bwd_kernel<T, 0>(s.warps, s.lanes, s.nv, full),
-                        a, s, st);
+  const NormKernel k = in ? bwd_kernel<T, 1>(s.warps, s.lanes, s.nv, full) : bwd_kernel<T, 0>(s.warps, s.lanes, s.nv, full);
+  bool ok = launch_dependent(k, static_cast<unsigned>(s.grid), 32u * s.warps, s.smem, st, 1, a) == cudaSuccess;
   ok = ok && launch_dependent(norm_reduce_kernel, static_cast<unsigned>(ceil_div(2 * C, 32)), 256, 0, st, 1,
                               static_cast<const float*>(part), s.grid, static_cast<int>(C), dgamma, dbeta) == cudaSuccess;
   return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
@@ -635,8 +632,7 @@ bool allow_rings() {
   for (int lanes = 8; lanes <= 32; lanes *= 2)
     for (int nv = 1; nv <= 4; ++nv)
       for (int full = 0; full < 2; ++full)
-        ok = ok && big_smem(fwd_kernel<T, 0>(lanes, nv, full)) && big_smem(fwd_kernel<T, 1>(lanes, nv, full)) &&
-             big_smem(fwd_kernel<T, 2>(lanes, nv, full)) && big_smem(bwd_kernel<T, 0>(BWD_WARPS, lanes, nv, full)) &&
+        ok = ok && big_smem(bwd_kernel<T, 0>(BWD_WARPS, lanes, nv, full)) &&
              big_smem(bwd_kernel<T, 1>(BWD_WARPS, lanes, nv, full)) && big_smem(bwd_kernel<T, 0>(WIDE_WARPS, lanes, nv, full)) &&
              big_smem(bwd_kernel<T, 1>(WIDE_WARPS, lanes, nv, full));
   return ok;

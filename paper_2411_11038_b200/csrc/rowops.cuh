@@ -56,6 +56,28 @@ __device__ __forceinline__ void unpack8(const uint4& r, const uint4& q, pair_t (
   v[2] = pair_of(q.x, q.y);
   v[3] = pair_of(q.z, q.w);
 }
+// 32 bytes at once, in one access where the address allows it (`wide`: 32-byte aligned).
+__device__ __forceinline__ void load32(const void* p, int wide, uint4& a, uint4& b) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                 : "l"(p));
+  } else {
+    a = reinterpret_cast<const uint4*>(p)[0];
+    b = reinterpret_cast<const uint4*>(p)[1];
+  }
+}
+__device__ __forceinline__ void store32(void* p, int wide, const uint4& a, const uint4& b) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z),
+                 "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = a;
+    reinterpret_cast<uint4*>(p)[1] = b;
+  }
+}
+
 template <typename T>
 struct Vec8;
 template <>
