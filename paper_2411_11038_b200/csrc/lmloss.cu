@@ -14,6 +14,10 @@
 // The logits of the backward are formed a second time from the stored lse: 2 of its 6 TVD
 // multiply-adds, instead of T V values kept from the forward.
 //
+// G lies in panels of 64 columns, each a dense [tokens x 64] matrix: a k-block of either product that reads
+// it is one contiguous piece of 16 KB.  (With plain rows, 128 of them contribute 128 bytes each to a
+// k-block of DH, and the product ran at 880 TFLOP/s.)
+//
 // G holds p - [v = label] times d_t / max|d|: the common factor max|d| is applied in fp32 behind the
 // products, so that the mean's 1 / n, the same for every token, costs no rounding.  Tokens without a
 // target (label < 0) are left out of the backward altogether: the tokens with one are gathered to
@@ -65,6 +69,7 @@ struct LmParams {
   float2* part; float* label_logit; int64_t part_pitch;
   // GRAD
   const TokenRow* rows; int v0;
+  int panel_rows;             // GRAD, DH, DW: rows of a 64-column panel of G (GRAD writes it, the others read it as A)
   // DH
   int first; int64_t slab_rows;
   // DW
@@ -202,8 +207,9 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
         const uint32_t fb = PAIR ? mapa_u32(smem_u32(&ctl->full[s]), 0) : 0u;
         if (A_MN && lane < 2) {
           uint8_t* dst = a_reg + lane * p.kps * CHUNK;
-          if (PAIR) tma_load_2d_pair(dst, &tmA, fb, m0 + 64 * lane, kb * KB);
-          else tma_load_2d(dst, &tmA, &ctl->full[s], m0 + 64 * lane, kb * KB);
+          const int y = (m0 / 64 + lane) * p.panel_rows + kb * KB;
+          if (PAIR) tma_load_2d_pair(dst, &tmA, fb, 0, y);
+          else tma_load_2d(dst, &tmA, &ctl->full[s], 0, y);
         }
         if (B_MN && lane >= 2 && lane - 2 < bn_cta / 64) {
           uint8_t* dst = b_reg + (lane - 2) * p.kps * CHUNK;
@@ -214,8 +220,9 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
         if (lane >= 8 && u < nsub) {
           if (!A_MN && !(lane & 1)) {
             uint8_t* dst = a_reg + u * A_KB_BYTES;
-            if (PAIR) tma_load_2d_pair(dst, &tmA, fb, (kb + u) * KB, m0);
-            else tma_load_2d(dst, &tmA, &ctl->full[s], (kb + u) * KB, m0);
+            const int x = EPI == LM_DH ? 0 : (kb + u) * KB, y = EPI == LM_DH ? (kb + u) * p.panel_rows + m0 : m0;
+            if (PAIR) tma_load_2d_pair(dst, &tmA, fb, x, y);
+            else tma_load_2d(dst, &tmA, &ctl->full[s], x, y);
           }
           if (!B_MN && (lane & 1)) {
             uint8_t* dst = b_reg + u * p.b_kb_bytes;
@@ -367,7 +374,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
       } else {
         for (int jb = jb0; jb < jb1; ++jb) {
           const int c0 = n0 + jb * BC;
-          if (c0 >= p.Nc) break;
+          if (c0 >= (EPI == LM_GRAD ? (p.Nc + 63) & ~int64_t(63) : p.Nc)) break;      // G: whole panels
           uint32_t r[32];
           if (BC == 32) tmem_ld_32x32(t_row + jb * BC, r); else tmem_ld_32x16(t_row + jb * BC, r);
           uint8_t* ob = my + (st_it & 1) * STG_BYTES;
@@ -384,6 +391,11 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (at == j) v[j] -= 1.f;
+            }
+            if (c0 + 32 > p.Nc) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (c0 + j >= p.Nc) v[j] = 0.f;      // past the vocabulary, up to the panel's end
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -413,7 +425,9 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
             if (EPI == LM_DH) {
               const int y = static_cast<int>(split * p.slab_rows) + row0;
               if (p.first) tma_store_2d(&tmOut, ob, c0, y); else tma_reduce_add_2d(&tmOut, ob, c0, y);
-            } else if (EPI == LM_GRAD || row0 < p.Mr) {
+            } else if (EPI == LM_GRAD) {
+              tma_store_2d(&tmOut, ob, c0 & 63, (c0 >> 6) * p.panel_rows + row0);
+            } else if (row0 < p.Mr) {
               tma_store_2d(&tmOut, ob, c0, row0);       // clipped at the tensor's edges
             }
             tma_store_commit();
@@ -574,16 +588,18 @@ struct Tiling {
   int64_t tiles_m, tiles_n;
 };
 
-// Tile shape of a product [rows x cols]: the one with the fewest tile times, where a tile of BN columns
-// costs BN + 24 (its epilogue and pipeline fill) and pairs of CTAs (256 rows, half the column operand's
-// traffic) are 8 % cheaper per column.  Column steps of `unit` (64 for MN-major operands).
+// Tile shape of a product [rows x cols]: the one with the fewest tile times.  A k-block of a 128-column tile
+// takes 0.33 us against 0.40 us of a 256-column one (pairs of CTAs, 256 rows, 8192 x 16128 x 2048): the
+// instruction takes 128 cycles whatever its width, and the row operand is loaded all the same.  Hence
+// 120 + 5/8 per column; tiles of one CTA, with half as much traffic again per multiplication, a quarter
+// more.  Column steps of `unit` (64 for MN-major operands).
 Tiling choose_tiling(int64_t rows, int64_t cols, int unit, int sm_count) {
   Tiling best = {};
   double cost = 1e300;
   if (rows > ROWS)
     for (int bn = 256; bn >= 128; bn >>= 1) {
       const int64_t tm = ceil_div(rows, 2 * ROWS), tn = ceil_div(cols, bn);
-      const double c = 0.92 * static_cast<double>(ceil_div(tm * tn, sm_count / 2)) * (bn + 24);
+      const double c = static_cast<double>(ceil_div(tm * tn, sm_count / 2)) * (120 + 0.625 * bn);
       if (c < cost) {
         cost = c;
         best = {1, bn, tm, tn};
@@ -591,7 +607,7 @@ Tiling choose_tiling(int64_t rows, int64_t cols, int unit, int sm_count) {
     }
   for (int bn = 256; bn >= 64; bn -= unit) {
     const int64_t tm = ceil_div(rows, ROWS), tn = ceil_div(cols, bn);
-    const double c = static_cast<double>(ceil_div(tm * tn, sm_count)) * (bn + 24);
+    const double c = 1.25 * static_cast<double>(ceil_div(tm * tn, sm_count)) * (120 + 0.625 * bn);
     if (c < cost) {
       cost = c;
       best = {0, bn, tm, tn};
@@ -781,7 +797,7 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     t.tiles_n = ceil_div(nv, t.BN);
     int rc = tensor_map_2d(&ta, w.Hc, 1, b.Tp, D, D, ROWS, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, t.pair ? t.BN / 2 : t.BN, 128);
-    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, w.G, 1, b.Tp, nv, b.Vc, 32, 64);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, 32, 64);
     if (rc != EFQAT_OK) return rc;
     LmParams p = {};
     p.Mr = T; p.Nc = nv;
@@ -790,20 +806,21 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     p.splits = 1;
     p.panel = panel_of(t, D);
     p.rows = w.rows; p.v0 = static_cast<int>(v0);
+    p.panel_rows = static_cast<int>(b.Tp);
     p.status = status;
     set_ring(&p, t, true);
     rc = launch<0, 0, LM_GRAD>(p, t, ta, tb, to, sm_count, st);
     if (rc != EFQAT_OK) return rc;
     // dH += G Wc
     t = b.dh;
-    rc = tensor_map_2d(&ta, w.G, 1, b.Tp, nv, b.Vc, ROWS, 128);
+    rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, ROWS, 128);
     p = LmParams{};
     p.Mr = T; p.Nc = D;
     p.n_rows = w.count;
     p.nkb = static_cast<int>(ceil_div(nv, KB));
     p.splits = b.splits < p.nkb ? b.splits : p.nkb;
     p.panel = static_cast<int>(t.tiles_n);
-    p.first = v0 == 0; p.slab_rows = b.Tp;
+    p.first = v0 == 0; p.slab_rows = b.Tp; p.panel_rows = static_cast<int>(b.Tp);
     p.status = status;
     set_ring(&p, t, true);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, KB * p.kps, 128);
@@ -821,7 +838,8 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     p.scale = w.scale;
     p.status = status;
     set_ring(&p, t, true);
-    rc = tensor_map_2d(&ta, w.G, 1, b.Tp, nv, b.Vc, KB * p.kps, 128);
+    p.panel_rows = static_cast<int>(b.Tp);
+    rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, KB * p.kps, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, w.Hc, 1, b.Tp, D, D, KB * p.kps, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&to, dW + v0 * D, 1, nv, D, D, 32, 64);
     if (rc == EFQAT_OK) rc = launch<1, 1, LM_DW>(p, t, ta, tb, to, sm_count, st);
