@@ -27,8 +27,7 @@
 // warp 0 = TMA producer over a ring of stages, warp 1 = tcgen05.mma issuer and TMEM owner,
 // warps 2..9 = epilogue (TMEM lane quarter x column half) on the other one of two accumulators.
 // A token is a row, i.e. a TMEM lane, i.e. a thread: the softmax statistics need no shuffle.
-#include "internal.h"
-#include "ptx.cuh"
+#include "rowops.cuh"
 
 namespace efqat {
 
@@ -63,7 +62,7 @@ struct LmParams {
   int nkb;                    // k-blocks (DW with n_rows: upper bound)
   int BN, kps, stages, splits;
   int panel;                  // tile columns walked row block by row block (order of the work list)
-  int b_kb_bytes;
+  int a_kb_tx, b_kb_bytes;    // bytes that a k-block's copies of A and of B bring
   // STAT
   const int32_t* labels;
   float2* part; float* label_logit; int64_t part_pitch;
@@ -74,6 +73,8 @@ struct LmParams {
   int first; int64_t slab_rows;
   // DW
   const float* scale;
+  // GRAD: G
+  bf16* out;
   int* status;
 };
 
@@ -117,7 +118,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int a_bytes = p.kps * A_KB_BYTES, b_bytes = p.kps * p.b_kb_bytes, stage_bytes = a_bytes + b_bytes;
   uint8_t* stg = smem + p.stages * stage_bytes;
-  Ctl* ctl = reinterpret_cast<Ctl*>(stg + (EPI == LM_STAT ? 0 : WORKERS * 2 * STG_BYTES));
+  Ctl* ctl = reinterpret_cast<Ctl*>(stg + (EPI == LM_DH || EPI == LM_DW ? WORKERS * 2 * STG_BYTES : 0));
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR ? static_cast<int>(cluster_ctarank()) : 0;
@@ -140,7 +141,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
     fence_barrier_init();
     prefetch_tmap(&tmA);
     prefetch_tmap(&tmB);
-    if (EPI != LM_STAT) prefetch_tmap(&tmOut);
+    if (EPI == LM_DH || EPI == LM_DW) prefetch_tmap(&tmOut);
   }
   if (warp == 1) {
     if (PAIR) {
@@ -193,7 +194,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
           } else if (rank == 0) {
             // the leader's barrier collects both CTAs' bytes; an MN-major box always brings all kps
             // k-blocks of its chunk
-            mbar_arrive_expect_tx(&ctl->full[s], (PAIR ? 2u : 1u) * (A_KB_BYTES * (A_MN ? p.kps : nsub) +
+            mbar_arrive_expect_tx(&ctl->full[s], (PAIR ? 2u : 1u) * (p.a_kb_tx * (A_MN ? p.kps : nsub) +
                                                                      p.b_kb_bytes * (B_MN ? p.kps : nsub)));
           }
         }
@@ -305,7 +306,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   } else {
     // ------------------------------------------------------------- epilogue
     const int e = warp - 2, q = warp & 3, half = e >> 2;
-    constexpr int BC = EPI == LM_DH ? 16 : 32;            // columns of a block: 64 bytes of output
+    constexpr int BC = EPI == LM_DH ? 16 : 32;            // columns of a block
     const int nblk = p.BN / BC, jb0 = half ? (nblk + 1) >> 1 : 0, jb1 = half ? nblk : (nblk + 1) >> 1;
     uint8_t* my = stg + e * 2 * STG_BYTES;
     int acc_it = 0, st_it = 0;
@@ -360,21 +361,59 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
             for (int j = 0; j < 32; ++j)
               if (at == j) p.label_logit[row] = __uint_as_float(r[j]);
           }
-          float top = __uint_as_float(r[0]);
+          // four chains each: a chain of 32 would be the epilogue's time on the last tile
+          float top[4], part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 1; j < 32; ++j) top = fmaxf(top, __uint_as_float(r[j]));
-          const float m1 = fmaxf(m, top), off = -m1 * LOG2E;
-          float part = 0.f;
+          for (int j = 0; j < 4; ++j) top[j] = __uint_as_float(r[j]);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) part += ex2(fmaf(__uint_as_float(r[j]), LOG2E, off));
-          sum = (m == -INFINITY ? 0.f : sum * ex2(fmaf(m, LOG2E, off))) + part;
+          for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(r[j]));
+          const float m1 = fmaxf(fmaxf(m, fmaxf(top[0], top[1])), fmaxf(top[2], top[3])), off = -m1 * LOG2E;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) part[j & 3] += ex2(fmaf(__uint_as_float(r[j]), LOG2E, off));
+          sum = (m == -INFINITY ? 0.f : sum * ex2(fmaf(m, LOG2E, off))) + ((part[0] + part[1]) + (part[2] + part[3]));
           m = m1;
         }
         if (live) p.part[static_cast<int64_t>(tn * 2 + half) * p.part_pitch + row] = make_float2(m, sum);
+      } else if (EPI == LM_GRAD) {
+        // A lane holds 32 columns of its row: two stores of 32 bytes into a panel, where the warp's rows are
+        // neighbours (a detour through shared memory and a bulk store cost 8 % of the product).
+        const int64_t cols = (p.Nc + 63) & ~int64_t(63);      // whole panels
+        for (int jb = jb0; jb < jb1; ++jb) {
+          const int c0 = n0 + jb * 32;
+          if (c0 >= cols) break;
+          uint32_t r[32];
+          tmem_ld_32x32(t_row + jb * 32, r);
+          tmem_wait_ld();
+          const int at = label - c0;
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(__uint_as_float(r[j]), LOG2E, nlse2));
+          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (at == j) v[j] -= 1.f;
+          }
+          if (c0 + 32 > p.Nc) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (c0 + j >= p.Nc) v[j] = 0.f;      // past the vocabulary, up to the panel's end
+          }
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = live ? v[j] * ratio : 0.f;
+          bf16* o = p.out + (static_cast<int64_t>(c0 >> 6) * p.panel_rows + row) * 64 + (c0 & 63);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            store32(o + 16 * i, 1,
+                    make_uint4(pack2(v[16 * i], v[16 * i + 1]), pack2(v[16 * i + 2], v[16 * i + 3]),
+                               pack2(v[16 * i + 4], v[16 * i + 5]), pack2(v[16 * i + 6], v[16 * i + 7])),
+                    make_uint4(pack2(v[16 * i + 8], v[16 * i + 9]), pack2(v[16 * i + 10], v[16 * i + 11]),
+                               pack2(v[16 * i + 12], v[16 * i + 13]), pack2(v[16 * i + 14], v[16 * i + 15])));
+        }
       } else {
+        // Rows far apart (dW), or a reduction (dH): 64 bytes of columns by 32 rows through a staging buffer.
         for (int jb = jb0; jb < jb1; ++jb) {
           const int c0 = n0 + jb * BC;
-          if (c0 >= (EPI == LM_GRAD ? (p.Nc + 63) & ~int64_t(63) : p.Nc)) break;      // G: whole panels
+          if (c0 >= p.Nc) break;
           uint32_t r[32];
           if (BC == 32) tmem_ld_32x32(t_row + jb * BC, r); else tmem_ld_32x16(t_row + jb * BC, r);
           uint8_t* ob = my + (st_it & 1) * STG_BYTES;
@@ -382,42 +421,17 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
           ++st_it;
           tmem_wait_ld();
           __syncwarp();
-          if (EPI == LM_GRAD) {
-            const int at = label - c0;
-            float v[32];
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(__uint_as_float(r[j]), LOG2E, nlse2));
-            if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (at == j) v[j] -= 1.f;
-            }
-            if (c0 + 32 > p.Nc) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c0 + j >= p.Nc) v[j] = 0.f;      // past the vocabulary, up to the panel's end
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float g[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) g[j] = live ? v[8 * i + j] * ratio : 0.f;
-              *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) =
-                  make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
-            }
-          } else if (EPI == LM_DW) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 4; ++i) {
+            if (EPI == LM_DW) {
               float g[8];
 #pragma unroll
               for (int j = 0; j < 8; ++j) g[j] = __uint_as_float(r[8 * i + j]) * out_scale;
               *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) =
                   make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
+            } else {
               *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+            }
           }
           fence_proxy_async();
           __syncwarp();
@@ -425,8 +439,6 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
             if (EPI == LM_DH) {
               const int y = static_cast<int>(split * p.slab_rows) + row0;
               if (p.first) tma_store_2d(&tmOut, ob, c0, y); else tma_reduce_add_2d(&tmOut, ob, c0, y);
-            } else if (EPI == LM_GRAD) {
-              tma_store_2d(&tmOut, ob, c0 & 63, (c0 >> 6) * p.panel_rows + row0);
             } else if (row0 < p.Mr) {
               tma_store_2d(&tmOut, ob, c0, row0);       // clipped at the tensor's edges
             }
@@ -441,7 +453,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
         else mbar_arrive(&ctl->acc_empty[buf]);
       }
     }
-    if (EPI != LM_STAT && lane == 0) tma_store_wait_all();
+    if ((EPI == LM_DH || EPI == LM_DW) && lane == 0) tma_store_wait_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -451,16 +463,16 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   }
 }
 
-// lse and loss of each token from the partial maxima and sums: 32 tokens per block, 8 threads each.
-__global__ void __launch_bounds__(256) lm_combine_kernel(const float2* __restrict__ part, int parts, int64_t pitch,
-                                                         const float* __restrict__ label_logit,
-                                                         const int32_t* __restrict__ labels, int64_t T, int64_t V,
-                                                         float* __restrict__ loss, float* __restrict__ lse, int* status) {
-  __shared__ float2 s[8][33];
+// lse and loss of each token from the partial maxima and sums: 16 tokens per block, 64 threads each.
+__global__ void __launch_bounds__(1024) lm_combine_kernel(const float2* __restrict__ part, int parts, int64_t pitch,
+                                                          const float* __restrict__ label_logit,
+                                                          const int32_t* __restrict__ labels, int64_t T, int64_t V,
+                                                          float* __restrict__ loss, float* __restrict__ lse, int* status) {
+  __shared__ float2 s[64][17];
   pdl_trigger();
   pdl_wait();
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * 32 + x;
+  const int x = threadIdx.x & 15, y = threadIdx.x >> 4;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * 16 + x;
   float m = -INFINITY, sum = 0.f;
   auto add = [&](float2 o) {
     const float m1 = fmaxf(m, o.x);
@@ -468,17 +480,36 @@ __global__ void __launch_bounds__(256) lm_combine_kernel(const float2* __restric
     sum = sum * ex2((m - m1) * LOG2E) + o.y * ex2((o.x - m1) * LOG2E);
     m = m1;
   };
-  if (t < T)
-    for (int i = y; i < parts; i += 8) add(part[static_cast<int64_t>(i) * pitch + t]);
+  if (t < T) {
+    for (int i = y; i < parts; i += 256) {
+      float2 o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        o[k] = i + 64 * k < parts ? part[static_cast<int64_t>(i + 64 * k) * pitch + t] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) add(o[k]);
+    }
+  }
   s[y][x] = make_float2(m, sum);
   __syncthreads();
-  if (y == 0 && t < T) {
-    for (int i = 1; i < 8; ++i) add(s[i][x]);
-    const float l = m + logf(sum);
-    const int label = labels[t];
-    lse[t] = l;
+  // token w of the block by warp w: a lane holds slices l and l + 32
+  const int w = threadIdx.x >> 5, l = threadIdx.x & 31;
+  const int64_t t2 = static_cast<int64_t>(blockIdx.x) * 16 + w;
+  if (w >= 16 || t2 >= T) return;
+  m = s[l][w].x;
+  sum = s[l][w].y;
+  add(s[l + 32][w]);
+  const float2 o = make_float2(m, sum);
+#pragma unroll
+  for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+  // (slices that saw nothing hold a zero sum; all of them -inf only where every logit is)
+  sum = warp_sum(o.y == 0.f ? 0.f : o.y * ex2((o.x - m) * LOG2E));
+  if (l == 0) {
+    const float z = m + logf(sum);
+    const int label = labels[t2];
+    lse[t2] = z;
     if (label >= V) record_status(status, EFQAT_DEV_BAD_INDEX);
-    loss[t] = label >= 0 && label < V ? l - label_logit[t] : 0.f;
+    loss[t2] = label >= 0 && label < V ? z - label_logit[t2] : 0.f;
   }
 }
 
@@ -561,24 +592,44 @@ __global__ void __launch_bounds__(256) lm_gather_kernel(const bf16* __restrict__
   }
 }
 
-// dH of every token: the slabs of its row summed in order, times max|dloss|, rounded once; zero without a target.
+// dH of every token: the slabs of its row summed in a fixed order, times max|dloss|, rounded once; zero
+// without a target.  A block takes 256 columns of a token: 64 lanes of 4 columns by 4 groups of slabs.
 __global__ void __launch_bounds__(256) lm_dh_kernel(const float* __restrict__ slabs, int splits, int64_t slab_rows,
                                                     const int* __restrict__ slot, const float* __restrict__ scale,
                                                     int64_t T, int D, bf16* __restrict__ dH) {
+  __shared__ float4 s_part[3][64];
   pdl_trigger();
   pdl_wait();
   const float f = *scale;
+  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int c = (blockIdx.y * 64 + x) * 4;
+  const int s0 = splits * y / 4, s1 = splits * (y + 1) / 4;
   for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
     const int i = slot[t];
-    for (int c = threadIdx.x * 4; c < D; c += 1024) {
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (i >= 0)
-        for (int s = 0; s < splits; ++s) {
-          const float4 a = *reinterpret_cast<const float4*>(slabs + (s * slab_rows + i) * D + c);
-          v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (i >= 0 && c < D)
+      for (int s = s0; s < s1; s += 8) {
+        float4 a[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          a[k] = s + k < s1 ? *reinterpret_cast<const float4*>(slabs + ((s + k) * slab_rows + i) * D + c)
+                            : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          v.x += a[k].x; v.y += a[k].y; v.z += a[k].z; v.w += a[k].w;
         }
+      }
+    if (y > 0) s_part[y - 1][x] = v;
+    __syncthreads();
+    if (y == 0 && c < D) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        const float4 a = s_part[k][x];
+        v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+      }
       *reinterpret_cast<uint2*>(dH + t * D + c) = make_uint2(pack2(v.x * f, v.y * f), pack2(v.z * f, v.w * f));
     }
+    __syncthreads();
   }
 }
 
@@ -597,7 +648,7 @@ Tiling choose_tiling(int64_t rows, int64_t cols, int unit, int sm_count) {
   Tiling best = {};
   double cost = 1e300;
   if (rows > ROWS)
-    for (int bn = 256; bn >= 128; bn >>= 1) {
+    for (int bn = 256; bn >= 128; bn -= unit == 64 ? 128 : unit) {
       const int64_t tm = ceil_div(rows, 2 * ROWS), tn = ceil_div(cols, bn);
       const double c = static_cast<double>(ceil_div(tm * tn, sm_count / 2)) * (120 + 0.625 * bn);
       if (c < cost) {
@@ -634,19 +685,24 @@ BwdPlan bwd_plan(int64_t T, int64_t V, int64_t D, int sm_count) {
   b.Vc = round_up(ceil_div(V, pieces), 256);
   b.grad = choose_tiling(T, b.Vc, 32, sm_count);
   b.dw = choose_tiling(b.Vc, D, 64, sm_count);
-  b.dh = choose_tiling(T, D, 64, sm_count);
-  // contraction split over the machine when dH has few tiles
-  const int units = b.dh.pair ? sm_count / 2 : sm_count;
-  const int64_t tiles = b.dh.tiles_m * b.dh.tiles_n, nkb = ceil_div(V < b.Vc ? V : b.Vc, KB);
+  // dH: tile shape and split of the contraction together, since it usually has fewer tiles than the machine
+  // has CTAs.  1 % per split for its slab of sums.
+  const int64_t nkb = ceil_div(V < b.Vc ? V : b.Vc, KB);
   double best = 1e300;
-  b.splits = 1;
-  for (int64_t c = 1; c <= units && c * 8 <= nkb && c * b.Tp * D * 4 <= PIECE_BYTES; ++c) {
-    const double cost = static_cast<double>(ceil_div(tiles * c, units)) / c * (1.0 + 0.01 * (c - 1));
-    if (cost < best - 1e-12) {
-      best = cost;
-      b.splits = static_cast<int>(c);
+  for (int pair = T > ROWS ? 1 : 0; pair >= 0; --pair)
+    for (int bn = 256; bn >= (pair ? 128 : 64); bn -= (pair ? 128 : 64)) {
+      const int64_t tm = ceil_div(T, pair ? 2 * ROWS : ROWS), tn = ceil_div(D, bn);
+      const int units = pair ? sm_count / 2 : sm_count;
+      for (int64_t c = 1; c <= units && (c == 1 || (c * 8 <= nkb && c * b.Tp * D * 4 <= PIECE_BYTES)); ++c) {
+        const double cost = (pair ? 1.0 : 1.25) * (120 + 0.625 * bn) *
+                            static_cast<double>(ceil_div(tm * tn * c, units)) / c * (1.0 + 0.01 * (c - 1));
+        if (cost < best - 1e-9) {
+          best = cost;
+          b.splits = static_cast<int>(c);
+          b.dh = {pair, bn, tm, tn};
+        }
+      }
     }
-  }
   return b;
 }
 
@@ -709,7 +765,7 @@ int launch(LmParams p, const Tiling& t, const CUtensorMap& ta, const CUtensorMap
   const int64_t items = t.tiles_m * t.tiles_n * p.splits;
   const int run = static_cast<int>(items < units ? items : units);
   const size_t smem = 1024 + static_cast<size_t>(p.stages) * p.kps * (A_KB_BYTES + bn_cta * 128) +
-                      (EPI == LM_STAT ? 0 : WORKERS * 2 * STG_BYTES) + sizeof(Ctl);
+                      (EPI == LM_DH || EPI == LM_DW ? WORKERS * 2 * STG_BYTES : 0) + sizeof(Ctl);
   count_launches(1);
   const cudaError_t e = t.pair
       ? launch_dependent(lm_kernel<A_MN, B_MN, EPI, 1>, 2u * run, THREADS, smem, st, 2, ta, tb, to, p)
@@ -717,8 +773,14 @@ int launch(LmParams p, const Tiling& t, const CUtensorMap& ta, const CUtensorMap
   return e == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
 
+// Rows of a token operand's box: with up to 128 tokens only those that exist (rounded to the swizzle's 8)
+// are copied; the other rows of the tile multiply whatever the stage holds into accumulator rows that
+// no epilogue reads as results.
+int token_box(int64_t T) { return T < ROWS ? static_cast<int>(round_up(T, 8)) : ROWS; }
+
 // Ring of the launch: stages of two k-blocks when three of them fit, else of one.
-void set_ring(LmParams* p, const Tiling& t, bool staging) {
+void set_ring(LmParams* p, const Tiling& t, bool staging, int a_rows) {
+  p->a_kb_tx = a_rows * KB * 2;
   const int bn_cta = t.pair ? t.BN / 2 : t.BN;
   p->b_kb_bytes = bn_cta * 128;
   const int sub = A_KB_BYTES + p->b_kb_bytes;
@@ -754,7 +816,7 @@ int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t
   const Tiling t = choose_tiling(T, V, 32, sm_count);
   const FwdWs w = carve_fwd(ws, T, t.tiles_n);
   CUtensorMap ta, tb;
-  int rc = tensor_map_2d(&ta, H, 1, T, D, D, ROWS, 128);
+  int rc = tensor_map_2d(&ta, H, 1, T, D, D, token_box(T), 128);
   if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, W, 1, V, D, D, t.pair ? t.BN / 2 : t.BN, 128);
   if (rc != EFQAT_OK) return rc;
   LmParams p = {};
@@ -765,11 +827,11 @@ int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t
   p.labels = labels;
   p.part = w.part; p.label_logit = w.label_logit; p.part_pitch = T;
   p.status = status;
-  set_ring(&p, t, false);
+  set_ring(&p, t, false, token_box(T));
   rc = launch<0, 0, LM_STAT>(p, t, ta, tb, ta, sm_count, st);
   if (rc != EFQAT_OK) return rc;
   count_launches(1);
-  return launch_dependent(lm_combine_kernel, static_cast<unsigned>(ceil_div(T, 32)), 256, 0, st, 1,
+  return launch_dependent(lm_combine_kernel, static_cast<unsigned>(ceil_div(T, 16)), 1024, 0, st, 1,
                           static_cast<const float2*>(w.part), static_cast<int>(2 * t.tiles_n), T,
                           static_cast<const float*>(w.label_logit), labels, T, V, loss, lse, status) == cudaSuccess
              ? EFQAT_OK : EFQAT_ERR_CUDA;
@@ -795,9 +857,8 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     // G = softmax gradient of this piece
     Tiling t = b.grad;
     t.tiles_n = ceil_div(nv, t.BN);
-    int rc = tensor_map_2d(&ta, w.Hc, 1, b.Tp, D, D, ROWS, 128);
+    int rc = tensor_map_2d(&ta, w.Hc, 1, b.Tp, D, D, token_box(T), 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, t.pair ? t.BN / 2 : t.BN, 128);
-    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, 32, 64);
     if (rc != EFQAT_OK) return rc;
     LmParams p = {};
     p.Mr = T; p.Nc = nv;
@@ -805,15 +866,16 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     p.nkb = static_cast<int>(ceil_div(D, KB));
     p.splits = 1;
     p.panel = panel_of(t, D);
+    p.out = w.G;
     p.rows = w.rows; p.v0 = static_cast<int>(v0);
     p.panel_rows = static_cast<int>(b.Tp);
     p.status = status;
-    set_ring(&p, t, true);
-    rc = launch<0, 0, LM_GRAD>(p, t, ta, tb, to, sm_count, st);
+    set_ring(&p, t, false, token_box(T));
+    rc = launch<0, 0, LM_GRAD>(p, t, ta, tb, ta, sm_count, st);
     if (rc != EFQAT_OK) return rc;
     // dH += G Wc
     t = b.dh;
-    rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, ROWS, 128);
+    rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, token_box(T), 128);
     p = LmParams{};
     p.Mr = T; p.Nc = D;
     p.n_rows = w.count;
@@ -822,7 +884,7 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     p.panel = static_cast<int>(t.tiles_n);
     p.first = v0 == 0; p.slab_rows = b.Tp; p.panel_rows = static_cast<int>(b.Tp);
     p.status = status;
-    set_ring(&p, t, true);
+    set_ring(&p, t, true, token_box(T));
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, KB * p.kps, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&to, w.slabs, 0, b.splits * b.Tp, D, D, 32, 64);
     if (rc == EFQAT_OK) rc = launch<0, 1, LM_DH>(p, t, ta, tb, to, sm_count, st);
@@ -837,7 +899,7 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     p.panel = static_cast<int>(t.tiles_n);
     p.scale = w.scale;
     p.status = status;
-    set_ring(&p, t, true);
+    set_ring(&p, t, true, ROWS);
     p.panel_rows = static_cast<int>(b.Tp);
     rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, KB * p.kps, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, w.Hc, 1, b.Tp, D, D, KB * p.kps, 128);
@@ -845,11 +907,22 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     if (rc == EFQAT_OK) rc = launch<1, 1, LM_DW>(p, t, ta, tb, to, sm_count, st);
     if (rc != EFQAT_OK) return rc;
   }
-  const unsigned grid = static_cast<unsigned>(T < sm_count * 8 ? T : sm_count * 8);
+  const int64_t slices = ceil_div(D, 256);
+  int64_t blocks = ceil_div(static_cast<int64_t>(sm_count) * 8, slices);
+  if (blocks > T) blocks = T;
   count_launches(1);
-  return launch_dependent(lm_dh_kernel, grid, 256u, 0, st, 1, static_cast<const float*>(w.slabs), b.splits, b.Tp,
-                          static_cast<const int*>(w.slot), static_cast<const float*>(w.scale), T, static_cast<int>(D),
-                          dH) == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(slices));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, lm_dh_kernel, static_cast<const float*>(w.slabs), b.splits, b.Tp,
+                            static_cast<const int*>(w.slot), static_cast<const float*>(w.scale), T, static_cast<int>(D),
+                            dH) == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
 
 }  // namespace efqat
