@@ -550,14 +550,23 @@ class QParamOptimizer:
 
 
 # ---------------------------------------------------------------------------------------
-# 8-bit activation checkpoints, GELU, layer norm
+# 8-bit activation checkpoints, GELU, layer norm, language-model loss.  These calls take a few microseconds on
+# small inputs, so what does not change from call to call (entry points, sizes, addresses of the plan's own
+# tensors) is marshalled once, when the plan is made.
+if _raw_stream is not None:
+    _stream_on = _raw_stream
+else:
+    def _stream_on(device: int) -> int:
+        return torch.cuda.current_stream(device).cuda_stream
+
+
 def _same(t: torch.Tensor, shape, dtype) -> int:
     """Device address of a tensor that must be a contiguous CUDA tensor of this shape and type."""
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype or tuple(t.shape) != shape:
         raise ValueError(f"expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous CUDA tensor")
-    return t.data_ptr()
+    raise ValueError("expected a contiguous CUDA tensor")
 
 
 def _code(dtype: torch.dtype) -> int:
@@ -568,6 +577,10 @@ def _code(dtype: torch.dtype) -> int:
     raise TypeError(f"activations must be fp32 or bf16, got {dtype}")
 
 
+def _own(t: torch.Tensor) -> C.c_void_p:
+    return C.c_void_p(t.data_ptr())
+
+
 class Checkpoint:
     """An activation [M,C] kept in 8 bits (efqat_ckpt): int8 codes and one fp32 scale per 128 elements of a
     row.  Written by store() or by the forward of LayerNormPlan / GeluPlan, read by load() or by their
@@ -576,29 +589,35 @@ class Checkpoint:
     GROUP = 128
 
     def __init__(self, ctx: Context, M: int, C_: int, device):
+        lib = load()
         nc, ns = C.c_size_t(0), C.c_size_t(0)
-        _check(load().efqat_ckpt_bytes(int(M), int(C_), C.byref(nc), C.byref(ns)), "efqat_ckpt_bytes")
+        _check(lib.efqat_ckpt_bytes(int(M), int(C_), C.byref(nc), C.byref(ns)), "efqat_ckpt_bytes")
         self.ctx, self.shape = ctx, (int(M), int(C_))
         self.nbytes = nc.value + ns.value
         self.codes = torch.empty(self.shape, dtype=torch.int8, device=device)
         self.scales = torch.empty((int(M), -(-int(C_) // self.GROUP)), dtype=torch.float32, device=device)
         self.arrays = CkptArrays(self.codes.data_ptr(), self.scales.data_ptr())
         self.ref = C.byref(self.arrays)
+        self._store, self._load, self._dims = lib.efqat_ckpt_store, lib.efqat_ckpt_load, (C.c_int64(M), C.c_int64(C_))
 
     def store(self, x: torch.Tensor) -> "Checkpoint":
         """efqat_ckpt_store."""
-        rc = load().efqat_ckpt_store(self.ctx.handle, _code(x.dtype), _same(x, self.shape, x.dtype), *self.shape,
-                                     self.ref, _stream())
-        _check(rc, "efqat_ckpt_store")
+        dt = x.dtype
+        rc = self._store(self.ctx.handle, _code(dt), _same(x, self.shape, dt), *self._dims, self.ref,
+                         _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_ckpt_store")
         return self
 
     def load(self, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """efqat_ckpt_load: the activation the checkpoint stands for, in `out` or a new tensor of `dtype`."""
         if out is None:
             out = torch.empty(self.shape, dtype=dtype, device=self.codes.device)
-        rc = load().efqat_ckpt_load(self.ctx.handle, _code(out.dtype), self.ref, *self.shape,
-                                    _same(out, self.shape, out.dtype), _stream())
-        _check(rc, "efqat_ckpt_load")
+        dt = out.dtype
+        rc = self._load(self.ctx.handle, _code(dt), self.ref, *self._dims, _same(out, self.shape, dt),
+                        _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_ckpt_load")
         return out
 
 
@@ -608,9 +627,7 @@ def _source(x: Optional[torch.Tensor], saved: Optional[Checkpoint], shape, dtype
         raise ValueError("give either x or its checkpoint")
     if saved is None:
         return _same(x, shape, dtype), None
-    if saved.shape != shape:
-        raise ValueError(f"checkpoint of shape {saved.shape}, expected {shape}")
-    return None, saved.ref
+    return None, _save(saved, shape)
 
 
 def _save(save: Optional[Checkpoint], shape):
@@ -625,30 +642,36 @@ class GeluPlan:
     """GELU over [M,C] activations; the output tensors are owned and reused by the plan."""
 
     def __init__(self, ctx: Context, M: int, C_: int, dtype: torch.dtype, device):
+        lib = load()
         self.ctx, self.shape, self.dtype, self.code = ctx, (int(M), int(C_)), dtype, _code(dtype)
         self.y = torch.empty(self.shape, dtype=dtype, device=device)
         self.dx = torch.empty(self.shape, dtype=dtype, device=device)
+        self._fwd, self._bwd, self._again = lib.efqat_gelu_fwd, lib.efqat_gelu_bwd, lib.efqat_gelu_recompute
+        self._dims, self._y, self._dx = (C.c_int64(M), C.c_int64(C_)), _own(self.y), _own(self.dx)
 
     def fwd(self, x: torch.Tensor, save: Optional[Checkpoint] = None) -> torch.Tensor:
         """efqat_gelu_fwd: y, and the checkpoint of x in `save` when given."""
-        rc = load().efqat_gelu_fwd(self.ctx.handle, self.code, _same(x, self.shape, self.dtype), *self.shape,
-                                   self.y.data_ptr(), _save(save, self.shape), _stream())
-        _check(rc, "efqat_gelu_fwd")
+        rc = self._fwd(self.ctx.handle, self.code, _same(x, self.shape, self.dtype), *self._dims, self._y,
+                       _save(save, self.shape), _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_gelu_fwd")
         return self.y
 
     def bwd(self, dy: torch.Tensor, x: Optional[torch.Tensor] = None, saved: Optional[Checkpoint] = None) -> torch.Tensor:
         """efqat_gelu_bwd: dx from dy and either x or its checkpoint."""
         px, ps = _source(x, saved, self.shape, self.dtype)
-        rc = load().efqat_gelu_bwd(self.ctx.handle, self.code, _same(dy, self.shape, self.dtype), px, ps, *self.shape,
-                                   self.dx.data_ptr(), _stream())
-        _check(rc, "efqat_gelu_bwd")
+        rc = self._bwd(self.ctx.handle, self.code, _same(dy, self.shape, self.dtype), px, ps, *self._dims, self._dx,
+                       _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_gelu_bwd")
         return self.dx
 
     def recompute(self, saved: Checkpoint) -> torch.Tensor:
         """efqat_gelu_recompute: y again, from the checkpoint."""
-        rc = load().efqat_gelu_recompute(self.ctx.handle, self.code, _save(saved, self.shape), *self.shape,
-                                         self.y.data_ptr(), _stream())
-        _check(rc, "efqat_gelu_recompute")
+        rc = self._again(self.ctx.handle, self.code, _save(saved, self.shape), *self._dims, self._y,
+                         _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_gelu_recompute")
         return self.y
 
 
@@ -664,14 +687,20 @@ class LayerNormPlan:
 
     def __init__(self, ctx: Context, M: int, C_: int, dtype: torch.dtype, device, eps: float = 1e-5,
                  backward: bool = True):
+        lib = load()
         self.ctx, self.shape, self.dtype, self.code, self.eps = ctx, (int(M), int(C_)), dtype, _code(dtype), float(eps)
         new = lambda *shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=device)
         self.param = (int(C_),)
         self.y = new(*self.shape, dt=dtype)
         self.mean, self.rstd = new(int(M)), new(int(M))
-        self.ws = alloc_workspace(layer_norm_workspace_bytes(M, C_), device)
+        ws_bytes = layer_norm_workspace_bytes(M, C_)
+        self._fwd, self._bwd, self._again = lib.efqat_layer_norm_fwd, lib.efqat_layer_norm_bwd, lib.efqat_layer_norm_recompute
+        self._dims, self._eps = (C.c_int64(M), C.c_int64(C_)), C.c_float(eps)
+        self._y, self._stats = _own(self.y), (_own(self.mean), _own(self.rstd))
         if backward:
+            self.ws = alloc_workspace(ws_bytes, device)
             self.dx, self.dgamma, self.dbeta = new(*self.shape, dt=dtype), new(int(C_)), new(int(C_))
+            self._grads = (_own(self.dx), _own(self.dgamma), _own(self.dbeta), _own(self.ws), C.c_size_t(self.ws.numel()))
 
     def _beta(self, beta):
         return None if beta is None else _same(beta, self.param, torch.float32)
@@ -679,30 +708,30 @@ class LayerNormPlan:
     def fwd(self, x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None,
             save: Optional[Checkpoint] = None) -> torch.Tensor:
         """efqat_layer_norm_fwd: y (and self.mean, self.rstd), and the checkpoint of x in `save` when given."""
-        rc = load().efqat_layer_norm_fwd(self.ctx.handle, self.code, _same(x, self.shape, self.dtype), *self.shape,
-                                         _same(gamma, self.param, torch.float32), self._beta(beta), self.eps,
-                                         self.y.data_ptr(), self.mean.data_ptr(), self.rstd.data_ptr(),
-                                         _save(save, self.shape), _stream())
-        _check(rc, "efqat_layer_norm_fwd")
+        rc = self._fwd(self.ctx.handle, self.code, _same(x, self.shape, self.dtype), *self._dims,
+                       _same(gamma, self.param, torch.float32), self._beta(beta), self._eps, self._y, *self._stats,
+                       _save(save, self.shape), _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_layer_norm_fwd")
         return self.y
 
     def bwd(self, dy: torch.Tensor, gamma: torch.Tensor, x: Optional[torch.Tensor] = None,
             saved: Optional[Checkpoint] = None):
         """efqat_layer_norm_bwd with the statistics of the last forward: dict(dx, dgamma, dbeta)."""
         px, ps = _source(x, saved, self.shape, self.dtype)
-        rc = load().efqat_layer_norm_bwd(self.ctx.handle, self.code, _same(dy, self.shape, self.dtype), px, ps,
-                                         *self.shape, _same(gamma, self.param, torch.float32), self.mean.data_ptr(),
-                                         self.rstd.data_ptr(), self.dx.data_ptr(), self.dgamma.data_ptr(),
-                                         self.dbeta.data_ptr(), self.ws.data_ptr(), self.ws.numel(), _stream())
-        _check(rc, "efqat_layer_norm_bwd")
+        rc = self._bwd(self.ctx.handle, self.code, _same(dy, self.shape, self.dtype), px, ps, *self._dims,
+                       _same(gamma, self.param, torch.float32), *self._stats, *self._grads, _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_layer_norm_bwd")
         return dict(dx=self.dx, dgamma=self.dgamma, dbeta=self.dbeta)
 
     def recompute(self, saved: Checkpoint, gamma: torch.Tensor, beta: Optional[torch.Tensor] = None) -> torch.Tensor:
         """efqat_layer_norm_recompute: y again, from the checkpoint and the statistics of the last forward."""
-        rc = load().efqat_layer_norm_recompute(self.ctx.handle, self.code, _save(saved, self.shape), *self.shape,
-                                               _same(gamma, self.param, torch.float32), self._beta(beta),
-                                               self.mean.data_ptr(), self.rstd.data_ptr(), self.y.data_ptr(), _stream())
-        _check(rc, "efqat_layer_norm_recompute")
+        rc = self._again(self.ctx.handle, self.code, _save(saved, self.shape), *self._dims,
+                         _same(gamma, self.param, torch.float32), self._beta(beta), *self._stats, self._y,
+                         _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_layer_norm_recompute")
         return self.y
 
 
@@ -719,32 +748,40 @@ class LmLossPlan:
     outputs and the workspace are owned and reused by the plan (lse of the last forward feeds its backward)."""
 
     def __init__(self, ctx: Context, T: int, V: int, D: int, device, backward: bool = True):
+        lib = load()
         self.ctx, self.dims = ctx, (int(T), int(V), int(D))
         self.h_shape, self.w_shape, self.t_shape = (int(T), int(D)), (int(V), int(D)), (int(T),)
         fwd, bwd = lm_loss_workspace_bytes(T, V, D)
         new = lambda shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=device)
         self.loss, self.lse = new(self.t_shape), new(self.t_shape)
         self.ws = alloc_workspace(max(fwd, bwd if backward else 0), device)
+        self._fwd, self._bwd = lib.efqat_lm_loss_fwd, lib.efqat_lm_loss_bwd
+        self._dims = tuple(C.c_int64(n) for n in self.dims)
+        self._lse, self._ws = _own(self.lse), (_own(self.ws), C.c_size_t(self.ws.numel()))
+        self._loss = _own(self.loss)
         if backward:
             self.dH, self.dW = new(self.h_shape, torch.bfloat16), new(self.w_shape, torch.bfloat16)
+            self._grads = (_own(self.dH), _own(self.dW))
+
+    def _inputs(self, H, W, labels):
+        return (_same(H, self.h_shape, torch.bfloat16), _same(W, self.w_shape, torch.bfloat16),
+                _same(labels, self.t_shape, torch.int32))
 
     def fwd(self, H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor) -> torch.Tensor:
         """efqat_lm_loss_fwd: the loss of each token, 0 where the label is negative (and self.lse)."""
-        rc = load().efqat_lm_loss_fwd(self.ctx.handle, _same(H, self.h_shape, torch.bfloat16),
-                                      _same(W, self.w_shape, torch.bfloat16), _same(labels, self.t_shape, torch.int32),
-                                      *self.dims, self.loss.data_ptr(), self.lse.data_ptr(), self.ws.data_ptr(),
-                                      self.ws.numel(), _stream())
-        _check(rc, "efqat_lm_loss_fwd")
+        rc = self._fwd(self.ctx.handle, *self._inputs(H, W, labels), *self._dims, self._loss, self._lse, *self._ws,
+                       _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_lm_loss_fwd")
         return self.loss
 
     def bwd(self, H: torch.Tensor, W: torch.Tensor, labels: torch.Tensor, dloss: torch.Tensor):
         """efqat_lm_loss_bwd with the lse of the last forward: dict(dH, dW)."""
-        rc = load().efqat_lm_loss_bwd(self.ctx.handle, _same(H, self.h_shape, torch.bfloat16),
-                                      _same(W, self.w_shape, torch.bfloat16), _same(labels, self.t_shape, torch.int32),
-                                      self.lse.data_ptr(), _same(dloss, self.t_shape, torch.float32), *self.dims,
-                                      self.dH.data_ptr(), self.dW.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
-                                      _stream())
-        _check(rc, "efqat_lm_loss_bwd")
+        rc = self._bwd(self.ctx.handle, *self._inputs(H, W, labels), self._lse,
+                       _same(dloss, self.t_shape, torch.float32), *self._dims, *self._grads, *self._ws,
+                       _stream_on(self.ctx.device))
+        if rc:
+            _check(rc, "efqat_lm_loss_bwd")
         return dict(dH=self.dH, dW=self.dW)
 
 
