@@ -513,124 +513,152 @@ __global__ void __launch_bounds__(1024) lm_combine_kernel(const float2* __restri
   }
 }
 
-// Tokens with a target, in order: token[i] and rows[i] for i < count, slot[t] = i or -1; and max|dloss| over
-// them (1 when it is zero or not finite: the ratios are then the gradients themselves).  One block; thread k
-// owns tokens [k seg, (k + 1) seg).
-__global__ void __launch_bounds__(1024) lm_compact_kernel(const int32_t* __restrict__ labels,
-                                                          const float* __restrict__ lse,
-                                                          const float* __restrict__ dloss, int T, int64_t V,
-                                                          int* __restrict__ count, float* __restrict__ scale,
-                                                          int* __restrict__ token, int* __restrict__ slot,
-                                                          TokenRow* __restrict__ rows, int* status) {
-  __shared__ int s_cnt[32];
-  __shared__ uint32_t s_max[32];
+// The tokens with a target, in order, moved to the front: rows[i] and their hidden states Hc[i] for i < count
+// (zeros up to the end of the last tile), slot[t] = i or -1; and max|dloss| over them (1 when it is zero or
+// not finite: the ratios are then the gradients themselves).  A block owns `per` consecutive tokens; every
+// block counts the tokens before its own and takes the maximum for itself (T is small beside T x D), so
+// that one launch does it all.
+__global__ void __launch_bounds__(256) lm_gather_kernel(const bf16* __restrict__ H, const int32_t* __restrict__ labels,
+                                                        const float* __restrict__ lse, const float* __restrict__ dloss,
+                                                        int T, int64_t V, int D, int64_t Dp, int per,
+                                                        int* __restrict__ count, float* __restrict__ scale,
+                                                        int* __restrict__ slot, TokenRow* __restrict__ rows,
+                                                        bf16* __restrict__ Hc, int* status) {
+  __shared__ int s_cnt[8], s_all[8], s_slot[256];
+  __shared__ uint32_t s_max[8];
   pdl_trigger();
   pdl_wait();
-  const int seg = (T + 1023) / 1024;
-  const int t0 = threadIdx.x * seg, t1 = t0 + seg < T ? t0 + seg : T;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int n = 0;
+  const int t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
+  int before = 0, all = 0;
   uint32_t top = 0;
-  for (int t = t0; t < t1; ++t) {
-    const int label = labels[t];
-    if (label >= V) record_status(status, EFQAT_DEV_BAD_INDEX);
-    if (label >= 0 && label < V) {
-      ++n;
-      top = max(top, __float_as_uint(dloss[t]) & 0x7fffffffu);
+  for (int tb = threadIdx.x; tb < T; tb += 2048) {
+    int label[8];
+    float d[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {      // 16 loads in flight
+      const int t = tb + 256 * k;
+      label[k] = t < T ? labels[t] : -1;
+      d[k] = t < T ? dloss[t] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (label[k] >= V && blockIdx.x == 0) record_status(status, EFQAT_DEV_BAD_INDEX);
+      if (label[k] >= 0 && label[k] < V) {
+        ++all;
+        before += tb + 256 * k < t0 ? 1 : 0;
+        top = max(top, __float_as_uint(d[k]) & 0x7fffffffu);
+      }
     }
   }
-  int incl = n;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += v;
+  for (int o = 16; o > 0; o >>= 1) {
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+    all += __shfl_xor_sync(0xffffffffu, all, o);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if (lane == 31) s_cnt[warp] = incl;
-  if (lane == 0) s_max[warp] = top;
+  if (lane == 0) {
+    s_cnt[warp] = before;
+    s_all[warp] = all;
+    s_max[warp] = top;
+  }
   __syncthreads();
-  int before = incl - n, total = 0;
-  uint32_t all = 0;
-  for (int w = 0; w < 32; ++w) {
-    if (w < warp) before += s_cnt[w];
-    total += s_cnt[w];
-    all = max(all, s_max[w]);
+  before = all = 0;
+  top = 0;
+  for (int w = 0; w < 8; ++w) {
+    before += s_cnt[w];
+    all += s_all[w];
+    top = max(top, s_max[w]);
   }
-  const float dmax = (all == 0 || all >= 0x7f800000u) ? 1.f : __uint_as_float(all);
-  for (int t = t0; t < t1; ++t) {
-    const int label = labels[t];
-    if (label >= 0 && label < V) {
-      TokenRow r;
-      r.nlse2 = -lse[t] * LOG2E;
-      r.ratio = __fdiv_rn(dloss[t], dmax);
-      r.label = label;
-      r.pad = 0;
-      rows[before] = r;
-      token[before] = t;
-      slot[t] = before++;
-    } else {
-      slot[t] = -1;
-    }
-  }
-  if (threadIdx.x == 0) {
-    *count = total;
+  const float dmax = (top == 0 || top >= 0x7f800000u) ? 1.f : __uint_as_float(top);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    *count = all;
     *scale = dmax;
   }
-}
-
-// Hidden states of the tokens with a target, gathered to the front; zeros up to the end of the last tile.
-__global__ void __launch_bounds__(256) lm_gather_kernel(const bf16* __restrict__ H, const int* __restrict__ count,
-                                                        const int* __restrict__ token, int D, bf16* __restrict__ Hc) {
-  pdl_trigger();
-  pdl_wait();
-  const int n = *count, end = ((n > 0 ? n : 1) + 255) & ~255;
-  for (int i = blockIdx.x; i < end; i += gridDim.x) {
-    const uint4* src = i < n ? reinterpret_cast<const uint4*>(H + static_cast<int64_t>(token[i]) * D) : nullptr;
-    uint4* dst = reinterpret_cast<uint4*>(Hc + static_cast<int64_t>(i) * D);
-    for (int c = threadIdx.x; c < D / 8; c += 256) dst[c] = src ? src[c] : make_uint4(0, 0, 0, 0);
+  // this block's tokens: their places, 256 at a time
+  for (int tb = t0; tb < t1; tb += 256) {
+    const int t = tb + threadIdx.x;
+    const int label = t < t1 ? labels[t] : -1;
+    const bool live = label >= 0 && label < V;
+    const uint32_t vote = __ballot_sync(0xffffffffu, live);
+    __syncthreads();
+    if (lane == 0) s_cnt[warp] = __popc(vote);
+    __syncthreads();
+    int at = before + __popc(vote & ((1u << lane) - 1));
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) at += s_cnt[w];
+      before += s_cnt[w];
+    }
+    if (t < t1) {
+      slot[t] = live ? at : -1;
+      if (live) {
+        TokenRow r;
+        r.nlse2 = -lse[t] * LOG2E;
+        r.ratio = __fdiv_rn(dloss[t], dmax);
+        r.label = label;
+        r.pad = 0;
+        rows[at] = r;
+      }
+    }
+    s_slot[threadIdx.x] = live ? at : -1;
+    __syncthreads();
+    const int n = t1 - tb < 256 ? t1 - tb : 256;
+    for (int k = warp; k < n; k += 8) {
+      const int i = s_slot[k];
+      if (i < 0) continue;
+      const uint4* src = reinterpret_cast<const uint4*>(H + static_cast<int64_t>(tb + k) * D);
+      uint4* dst = reinterpret_cast<uint4*>(Hc + static_cast<int64_t>(i) * Dp);
+      for (int c = lane; c < D / 8; c += 32) dst[c] = src[c];
+    }
+  }
+  // zeros from the last token to the end of its tile, shared among the blocks
+  const int end = ((all > 0 ? all : 1) + 255) & ~255;
+  for (int i = all + blockIdx.x * 8 + warp; i < end; i += gridDim.x * 8) {
+    uint4* dst = reinterpret_cast<uint4*>(Hc + static_cast<int64_t>(i) * Dp);
+    for (int c = lane; c < D / 8; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
   }
 }
 
 // dH of every token: the slabs of its row summed in a fixed order, times max|dloss|, rounded once; zero
-// without a target.  A block takes 256 columns of a token: 64 lanes of 4 columns by 4 groups of slabs.
+// without a target.  A thread takes 4 columns; with many slabs (few tokens) GROUPS threads share them.
+template <int GROUPS>
 __global__ void __launch_bounds__(256) lm_dh_kernel(const float* __restrict__ slabs, int splits, int64_t slab_rows,
                                                     const int* __restrict__ slot, const float* __restrict__ scale,
-                                                    int64_t T, int D, bf16* __restrict__ dH) {
-  __shared__ float4 s_part[3][64];
+                                                    int slices, int D, bf16* __restrict__ dH) {
+  constexpr int LANES = 256 / GROUPS;
+  __shared__ float4 s_part[GROUPS][LANES];
   pdl_trigger();
   pdl_wait();
+  const int64_t t = blockIdx.x / slices;
+  const int x = threadIdx.x % LANES, y = threadIdx.x / LANES;
+  const int c = ((blockIdx.x % slices) * LANES + x) * 4;
+  const int s0 = splits * y / GROUPS, s1 = splits * (y + 1) / GROUPS;
+  const int i = slot[t];
   const float f = *scale;
-  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-  const int c = (blockIdx.y * 64 + x) * 4;
-  const int s0 = splits * y / 4, s1 = splits * (y + 1) / 4;
-  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-    const int i = slot[t];
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (i >= 0 && c < D)
-      for (int s = s0; s < s1; s += 8) {
-        float4 a[8];
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (i >= 0 && c < D)
+    for (int s = s0; s < s1; s += 4) {
+      float4 a[4];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          a[k] = s + k < s1 ? *reinterpret_cast<const float4*>(slabs + ((s + k) * slab_rows + i) * D + c)
-                            : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < 4; ++k)
+        a[k] = s + k < s1 ? *reinterpret_cast<const float4*>(slabs + ((s + k) * slab_rows + i) * D + c)
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          v.x += a[k].x; v.y += a[k].y; v.z += a[k].z; v.w += a[k].w;
-        }
+      for (int k = 0; k < 4; ++k) {
+        v.x += a[k].x; v.y += a[k].y; v.z += a[k].z; v.w += a[k].w;
       }
-    if (y > 0) s_part[y - 1][x] = v;
-    __syncthreads();
-    if (y == 0 && c < D) {
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        const float4 a = s_part[k][x];
-        v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
-      }
-      *reinterpret_cast<uint2*>(dH + t * D + c) = make_uint2(pack2(v.x * f, v.y * f), pack2(v.z * f, v.w * f));
     }
+  if (GROUPS > 1) {
+    s_part[y][x] = v;
     __syncthreads();
+    if (y > 0) return;
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) {
+      const float4 a = s_part[k][x];
+      v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+    }
   }
+  if (c < D) *reinterpret_cast<uint2*>(dH + t * D + c) = make_uint2(pack2(v.x * f, v.y * f), pack2(v.z * f, v.w * f));
 }
 
 // ------------------------------------------------------------------ host side
@@ -670,7 +698,7 @@ Tiling choose_tiling(int64_t rows, int64_t cols, int unit, int sm_count) {
 static const int64_t PIECE_BYTES = 256ll << 20;      // most bytes of G at a time
 
 struct BwdPlan {
-  int64_t Tp, Vc;      // padded tokens; vocabulary columns of a piece
+  int64_t Tp, Vc, Dp;  // padded tokens; vocabulary columns of a piece; row pitch of the gathered hidden states
   int splits;
   Tiling grad, dh, dw;
 };
@@ -678,6 +706,7 @@ struct BwdPlan {
 BwdPlan bwd_plan(int64_t T, int64_t V, int64_t D, int sm_count) {
   BwdPlan b = {};
   b.Tp = round_up(T, 256);
+  b.Dp = round_up(D, 64);      // rows start on a 128-byte line whatever D is
   // pieces of equal size, whole tiles wide
   int64_t most = PIECE_BYTES / (2 * b.Tp) / 256 * 256;
   if (most < 256) most = 256;
@@ -726,7 +755,7 @@ FwdWs carve_fwd(void* ws, int64_t T, int64_t tiles_n) {
 }
 
 struct BwdWs {
-  bf16* Hc; bf16* G; float* slabs; TokenRow* rows; int* token; int* slot; int* count; float* scale;
+  bf16* Hc; bf16* G; float* slabs; TokenRow* rows; int* slot; int* count; float* scale;
   size_t bytes;
 };
 BwdWs carve_bwd(void* ws, const BwdPlan& b, int64_t T, int64_t D) {
@@ -738,11 +767,10 @@ BwdWs carve_bwd(void* ws, const BwdPlan& b, int64_t T, int64_t D) {
     off += static_cast<size_t>(round_up(bytes, 256));
     return r;
   };
-  w.Hc = reinterpret_cast<bf16*>(take(b.Tp * D * 2));
+  w.Hc = reinterpret_cast<bf16*>(take(b.Tp * b.Dp * 2));
   w.G = reinterpret_cast<bf16*>(take(b.Tp * b.Vc * 2));
   w.slabs = reinterpret_cast<float*>(take(b.splits * b.Tp * D * 4));
   w.rows = reinterpret_cast<TokenRow*>(take(b.Tp * 16));
-  w.token = reinterpret_cast<int*>(take(T * 4));
   w.slot = reinterpret_cast<int*>(take(T * 4));
   w.count = reinterpret_cast<int*>(take(4));
   w.scale = reinterpret_cast<float*>(take(4));
@@ -842,14 +870,14 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
                     cudaStream_t st) {
   const BwdPlan b = bwd_plan(T, V, D, sm_count);
   const BwdWs w = carve_bwd(ws, b, T, D);
-  bool ok = true;
-  count_launches(2);
-  ok = ok && launch_dependent(lm_compact_kernel, 1u, 1024u, 0, st, 1, labels, lse, dloss, static_cast<int>(T), V,
-                              w.count, w.scale, w.token, w.slot, w.rows, status) == cudaSuccess;
-  const unsigned gather = static_cast<unsigned>(b.Tp < sm_count * 8 ? b.Tp : sm_count * 8);
-  ok = ok && launch_dependent(lm_gather_kernel, gather, 256u, 0, st, 1, H, static_cast<const int*>(w.count),
-                              static_cast<const int*>(w.token), static_cast<int>(D), w.Hc) == cudaSuccess;
-  if (!ok) return EFQAT_ERR_CUDA;
+  // 8 tokens to a block (a warp each), more where that would be more than 8 blocks per SM
+  int64_t per = ceil_div(T, static_cast<int64_t>(sm_count) * 8);
+  if (per < 8) per = 8;
+  count_launches(1);
+  if (launch_dependent(lm_gather_kernel, static_cast<unsigned>(ceil_div(T, per)), 256u, 0, st, 1, H, labels, lse, dloss,
+                       static_cast<int>(T), V, static_cast<int>(D), b.Dp, static_cast<int>(per), w.count, w.scale, w.slot,
+                       w.rows, w.Hc, status) != cudaSuccess)
+    return EFQAT_ERR_CUDA;
   for (int64_t v0 = 0; v0 < V; v0 += b.Vc) {
     const int64_t nv = V - v0 < b.Vc ? V - v0 : b.Vc;
     const bf16* Wc = W + v0 * D;
@@ -857,7 +885,7 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     // G = softmax gradient of this piece
     Tiling t = b.grad;
     t.tiles_n = ceil_div(nv, t.BN);
-    int rc = tensor_map_2d(&ta, w.Hc, 1, b.Tp, D, D, token_box(T), 128);
+    int rc = tensor_map_2d(&ta, w.Hc, 1, b.Tp, D, b.Dp, token_box(T), 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, Wc, 1, nv, D, D, t.pair ? t.BN / 2 : t.BN, 128);
     if (rc != EFQAT_OK) return rc;
     LmParams p = {};
@@ -902,27 +930,18 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     set_ring(&p, t, true, ROWS);
     p.panel_rows = static_cast<int>(b.Tp);
     rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, KB * p.kps, 128);
-    if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, w.Hc, 1, b.Tp, D, D, KB * p.kps, 128);
+    if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, w.Hc, 1, b.Tp, D, b.Dp, KB * p.kps, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&to, dW + v0 * D, 1, nv, D, D, 32, 64);
     if (rc == EFQAT_OK) rc = launch<1, 1, LM_DW>(p, t, ta, tb, to, sm_count, st);
     if (rc != EFQAT_OK) return rc;
   }
-  const int64_t slices = ceil_div(D, 256);
-  int64_t blocks = ceil_div(static_cast<int64_t>(sm_count) * 8, slices);
-  if (blocks > T) blocks = T;
+  const int groups = b.splits >= 8 ? 8 : 1;
+  const int slices = static_cast<int>(ceil_div(D, 1024 / groups));
   count_launches(1);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(slices));
-  cfg.blockDim = dim3(256);
-  cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, lm_dh_kernel, static_cast<const float*>(w.slabs), b.splits, b.Tp,
-                            static_cast<const int*>(w.slot), static_cast<const float*>(w.scale), T, static_cast<int>(D),
-                            dH) == cudaSuccess ? EFQAT_OK : EFQAT_ERR_CUDA;
+  return launch_dependent(groups == 8 ? lm_dh_kernel<8> : lm_dh_kernel<1>, static_cast<unsigned>(T * slices), 256u, 0, st, 1,
+                          static_cast<const float*>(w.slabs), b.splits, b.Tp, static_cast<const int*>(w.slot),
+                          static_cast<const float*>(w.scale), slices, static_cast<int>(D), dH) == cudaSuccess
+             ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
 
 }  // namespace efqat

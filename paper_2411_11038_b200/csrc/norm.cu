@@ -196,6 +196,16 @@ struct Raw {
       if (sizeof(T) == 4) r[sizeof(r) / 16 - 1] = p[1];
     }
   }
+  __device__ __forceinline__ void load_shared(uint32_t addr) {
+    if (SRC) {
+      const uint2 w = lds64(addr);
+      r[0].x = w.x;
+      r[0].y = w.y;
+    } else {
+      r[0] = lds128(addr);
+      if (sizeof(T) == 4) r[sizeof(r) / 16 - 1] = lds128(addr + 16);
+    }
+  }
   __device__ __forceinline__ void get(float scale, pair_t (&v)[4]) const {
     if (SRC) ckpt_values(make_uint2(r[0].x, r[0].y), scale, v);
     else if (sizeof(T) == 2) unpack8(r[0], v);
@@ -203,7 +213,8 @@ struct Raw {
   }
   // From here on the elements are unpacked anew: their unpacked values are not worth registers.
   __device__ __forceinline__ void forget() {
-    if (sizeof(T) == 2) asm volatile("" : "+r"(r[0].x), "+r"(r[0].y), "+r"(r[0].z), "+r"(r[0].w));
+    if (SRC) asm volatile("" : "+r"(r[0].x), "+r"(r[0].y));
+    else if (sizeof(T) == 2) asm volatile("" : "+r"(r[0].x), "+r"(r[0].y), "+r"(r[0].z), "+r"(r[0].w));
   }
   __device__ __forceinline__ uint32_t top() const {
     return max(ckpt_top(r[0], T()), ckpt_top(r[sizeof(r) / 16 - 1], T()));
@@ -489,24 +500,26 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_bwd_kernel(NormArgs a) {
   }
 }
 
-// dgamma / dbeta: columns of the [parts][2 C] partial sums.  8 threads per column, fixed order.
-__global__ void __launch_bounds__(256) norm_reduce_kernel(const float* __restrict__ part, int parts, int C,
-                                                          float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float s[8][33];
+// dgamma / dbeta: columns of the [parts][2 C] partial sums.  32 threads per column, fixed order.
+__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* __restrict__ part, int parts, int C,
+                                                           float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float s[32][33];
   pdl_trigger();
   pdl_wait();
   const int cx = threadIdx.x & 31, ry = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + cx;
   float t = 0.f;
   if (c < 2 * C) {
-#pragma unroll 8
-    for (int r = ry; r < parts; r += 8) t += part[static_cast<int64_t>(r) * 2 * C + c];
+#pragma unroll 5
+    for (int r = ry; r < parts; r += 32) t += part[static_cast<int64_t>(r) * 2 * C + c];
   }
   s[ry][cx] = t;
   __syncthreads();
-  if (ry == 0 && c < 2 * C) {
-    for (int r = 1; r < 8; ++r) t += s[r][cx];
-    if (c < C) dgamma[c] = t; else dbeta[c - C] = t;
+  // column ry of the block by warp ry
+  const int c2 = blockIdx.x * 32 + ry;
+  t = warp_sum(s[cx][ry]);
+  if (cx == 0 && c2 < 2 * C) {
+    if (c2 < C) dgamma[c2] = t; else dbeta[c2 - C] = t;
   }
 }
 
@@ -618,7 +631,7 @@ int bwd_t(const void* dy, const void* x, const efqat_ckpt* in, int64_t M, int64_
   const bool full = s.lanes == 32 && C == 256 * s.nv * s.team;
   const NormKernel k = in ? bwd_kernel<T, 1>(s.warps, s.lanes, s.nv, full) : bwd_kernel<T, 0>(s.warps, s.lanes, s.nv, full);
   bool ok = launch_dependent(k, static_cast<unsigned>(s.grid), 32u * s.warps, s.smem, st, 1, a) == cudaSuccess;
-  ok = ok && launch_dependent(norm_reduce_kernel, static_cast<unsigned>(ceil_div(2 * C, 32)), 256, 0, st, 1,
+  ok = ok && launch_dependent(norm_reduce_kernel, static_cast<unsigned>(ceil_div(2 * C, 32)), 1024, 0, st, 1,
                               static_cast<const float*>(part), s.grid, static_cast<int>(C), dgamma, dbeta) == cudaSuccess;
   return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
