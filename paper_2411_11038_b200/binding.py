@@ -683,23 +683,28 @@ def layer_norm_workspace_bytes(M: int, C_: int) -> int:
 
 class LayerNormPlan:
     """Layer norm over the rows of [M,C] activations; outputs, statistics and workspace are owned and reused
-    by the plan (y, mean, rstd of the last forward; dx, dgamma, dbeta of the last backward)."""
+    by the plan (y, mean, rstd of the last forward; dx, dgamma, dbeta of the last backward).  outputs: another
+    plan of the same shape whose y, dx and workspace this one uses (the statistics and the parameters'
+    gradients stay its own): layers of a stack that keep a checkpoint of their input need no more."""
 
     def __init__(self, ctx: Context, M: int, C_: int, dtype: torch.dtype, device, eps: float = 1e-5,
-                 backward: bool = True):
+                 backward: bool = True, outputs: Optional["LayerNormPlan"] = None):
         lib = load()
         self.ctx, self.shape, self.dtype, self.code, self.eps = ctx, (int(M), int(C_)), dtype, _code(dtype), float(eps)
         new = lambda *shape, dt=torch.float32: torch.empty(shape, dtype=dt, device=device)
         self.param = (int(C_),)
-        self.y = new(*self.shape, dt=dtype)
+        if outputs is not None and (outputs.shape, outputs.dtype) != (self.shape, dtype):
+            raise ValueError("output tensors can only be shared between plans of one shape")
+        self.y = new(*self.shape, dt=dtype) if outputs is None else outputs.y
         self.mean, self.rstd = new(int(M)), new(int(M))
         ws_bytes = layer_norm_workspace_bytes(M, C_)
         self._fwd, self._bwd, self._again = lib.efqat_layer_norm_fwd, lib.efqat_layer_norm_bwd, lib.efqat_layer_norm_recompute
         self._dims, self._eps = (C.c_int64(M), C.c_int64(C_)), C.c_float(eps)
         self._y, self._stats = _own(self.y), (_own(self.mean), _own(self.rstd))
         if backward:
-            self.ws = alloc_workspace(ws_bytes, device)
-            self.dx, self.dgamma, self.dbeta = new(*self.shape, dt=dtype), new(int(C_)), new(int(C_))
+            self.ws = alloc_workspace(ws_bytes, device) if outputs is None else outputs.ws
+            self.dx = new(*self.shape, dt=dtype) if outputs is None else outputs.dx
+            self.dgamma, self.dbeta = new(int(C_)), new(int(C_))
             self._grads = (_own(self.dx), _own(self.dgamma), _own(self.dbeta), _own(self.ws), C.c_size_t(self.ws.numel()))
 
     def _beta(self, beta):

@@ -5,7 +5,7 @@
 // 8 registers and 4 shuffles, its codes leave as one 8-byte store per lane.
 #pragma once
 #include "internal.h"
-#include "ptx.cuh"
+#include "async.cuh"
 
 namespace efqat {
 
