@@ -32,6 +32,12 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   return r;
 }
 
+// Arrives on a barrier of a CTA of this cluster without ordering memory beyond the CTA (a release at cluster
+// scope waits for the thread's global stores): for a hand-over that carries no data in memory.
+__device__ __forceinline__ void mbar_arrive_peer(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
 // Barrier `id` (1..15) over `threads` threads of the block.
 __device__ __forceinline__ void named_barrier(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");

@@ -73,8 +73,7 @@ struct LmParams {
   int first; int64_t slab_rows;
   // DW
   const float* scale;
-  // GRAD: G
-  bf16* out;
+  bf16* out;                  // GRAD: G; DW: rows of dW
   int* status;
 };
 
@@ -98,6 +97,11 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // 16-byte piece `piece` of row `row` of a 64-byte-swizzled staging block.
 __device__ __forceinline__ uint8_t* stg_addr(uint8_t* base, int row, int piece) {
   return base + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4);
+}
+
+// ... and of a block of 32 lines of 128 bytes.
+__device__ __forceinline__ uint8_t* line_addr(uint8_t* base, int row, int piece) {
+  return base + row * 128 + ((piece ^ (row & 7)) << 4);
 }
 
 // Tile t of the work list: panels of `panel` tile columns; inside a panel row block by row block.
@@ -141,7 +145,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
     fence_barrier_init();
     prefetch_tmap(&tmA);
     prefetch_tmap(&tmB);
-    if (EPI == LM_DH || EPI == LM_DW) prefetch_tmap(&tmOut);
+    if (EPI == LM_DH) prefetch_tmap(&tmOut);
   }
   if (warp == 1) {
     if (PAIR) {
@@ -306,7 +310,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   } else {
     // ------------------------------------------------------------- epilogue
     const int e = warp - 2, q = warp & 3, half = e >> 2;
-    constexpr int BC = EPI == LM_DH ? 16 : 32;            // columns of a block
+    constexpr int BC = EPI == LM_DH ? 16 : EPI == LM_DW ? 64 : 32;      // columns of a block
     const int nblk = p.BN / BC, jb0 = half ? (nblk + 1) >> 1 : 0, jb1 = half ? nblk : (nblk + 1) >> 1;
     uint8_t* my = stg + e * 2 * STG_BYTES;
     int acc_it = 0, st_it = 0;
@@ -342,6 +346,19 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
       }
       tc_fence_after();
       const uint32_t t_row = tmem_base + buf * ACC_COLS + (static_cast<uint32_t>(q * 32) << 16);
+      // Hands the accumulator back, once this warp's last columns are in registers.
+      bool released = false;
+      auto release = [&]() {
+        released = true;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) mbar_arrive_peer(mapa_u32(smem_u32(&ctl->acc_empty[buf]), 0));
+          else mbar_arrive(&ctl->acc_empty[buf]);
+        }
+      };
+      const int64_t cols = EPI == LM_GRAD ? (p.Nc + 63) & ~int64_t(63) : p.Nc;      // G: whole panels
+      auto last_block = [&](int jb) { return jb + 1 == jb1 || n0 + (jb + 1) * BC >= cols; };
       if (EPI == LM_STAT) {
         float m = -INFINITY, sum = 0.f;
         for (int jb = jb0; jb < jb1; ++jb) {
@@ -350,6 +367,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
           uint32_t r[32];
           tmem_ld_32x32(t_row + jb * 32, r);
           tmem_wait_ld();
+          if (last_block(jb)) release();
           if (c0 + 32 > p.Nc) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
@@ -377,13 +395,13 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
       } else if (EPI == LM_GRAD) {
         // A lane holds 32 columns of its row: two stores of 32 bytes into a panel, where the warp's rows are
         // neighbours (a detour through shared memory and a bulk store cost 8 % of the product).
-        const int64_t cols = (p.Nc + 63) & ~int64_t(63);      // whole panels
         for (int jb = jb0; jb < jb1; ++jb) {
           const int c0 = n0 + jb * 32;
           if (c0 >= cols) break;
           uint32_t r[32];
           tmem_ld_32x32(t_row + jb * 32, r);
           tmem_wait_ld();
+          if (last_block(jb)) release();
           const int at = label - c0;
           float v[32];
 #pragma unroll
@@ -409,51 +427,65 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
                     make_uint4(pack2(v[16 * i + 8], v[16 * i + 9]), pack2(v[16 * i + 10], v[16 * i + 11]),
                                pack2(v[16 * i + 12], v[16 * i + 13]), pack2(v[16 * i + 14], v[16 * i + 15])));
         }
-      } else {
-        // Rows far apart (dW), or a reduction (dH): 64 bytes of columns by 32 rows through a staging buffer.
+      } else if (EPI == LM_DW) {
+        // Rows far apart: 64 columns by 32 rows are turned in shared memory and leave as whole 128-byte lines.
         for (int jb = jb0; jb < jb1; ++jb) {
-          const int c0 = n0 + jb * BC;
+          const int c0 = n0 + jb * 64;
+          if (c0 >= p.Nc) break;
+          uint32_t r[2][32];
+          tmem_ld_32x32(t_row + jb * 64, r[0]);
+          tmem_ld_32x32(t_row + jb * 64 + 32, r[1]);
+          tmem_wait_ld();
+          if (last_block(jb)) release();
+          __syncwarp();      // the lines of the block before this one have been read
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float g[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) g[j] = __uint_as_float(r[h][8 * i + j]) * out_scale;
+              *reinterpret_cast<uint4*>(line_addr(my, lane, 4 * h + i)) =
+                  make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
+            }
+          __syncwarp();
+          const int col = c0 + (lane & 7) * 8;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int rr = 4 * i + (lane >> 3);
+            const uint4 q = *reinterpret_cast<const uint4*>(line_addr(my, rr, lane & 7));
+            if (row0 + rr < p.Mr && col < p.Nc)
+              *reinterpret_cast<uint4*>(p.out + static_cast<int64_t>(row0 + rr) * p.Nc + col) = q;
+          }
+        }
+      } else {
+        // dH: 64 bytes of columns by 32 rows through a staging buffer, added in L2.
+        for (int jb = jb0; jb < jb1; ++jb) {
+          const int c0 = n0 + jb * 16;
           if (c0 >= p.Nc) break;
           uint32_t r[32];
-          if (BC == 32) tmem_ld_32x32(t_row + jb * BC, r); else tmem_ld_32x16(t_row + jb * BC, r);
+          tmem_ld_32x16(t_row + jb * 16, r);
           uint8_t* ob = my + (st_it & 1) * STG_BYTES;
           if (lane == 0) tma_store_wait_read1();      // the store that last used this buffer has read it
           ++st_it;
           tmem_wait_ld();
+          if (last_block(jb)) release();
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (EPI == LM_DW) {
-              float g[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) g[j] = __uint_as_float(r[8 * i + j]) * out_scale;
-              *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) =
-                  make_uint4(pack2(g[0], g[1]), pack2(g[2], g[3]), pack2(g[4], g[5]), pack2(g[6], g[7]));
-            } else {
-              *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
-            }
-          }
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(stg_addr(ob, lane, i)) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
-            if (EPI == LM_DH) {
-              const int y = static_cast<int>(split * p.slab_rows) + row0;
-              if (p.first) tma_store_2d(&tmOut, ob, c0, y); else tma_reduce_add_2d(&tmOut, ob, c0, y);
-            } else if (row0 < p.Mr) {
-              tma_store_2d(&tmOut, ob, c0, row0);       // clipped at the tensor's edges
-            }
+            const int y = static_cast<int>(split * p.slab_rows) + row0;
+            if (p.first) tma_store_2d(&tmOut, ob, c0, y); else tma_reduce_add_2d(&tmOut, ob, c0, y);
             tma_store_commit();
           }
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) mbar_arrive_cluster(mapa_u32(smem_u32(&ctl->acc_empty[buf]), 0));
-        else mbar_arrive(&ctl->acc_empty[buf]);
-      }
+      if (!released) release();
     }
-    if ((EPI == LM_DH || EPI == LM_DW) && lane == 0) tma_store_wait_all();
+    if (EPI == LM_DH && lane == 0) tma_store_wait_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -931,8 +963,8 @@ int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const f
     p.panel_rows = static_cast<int>(b.Tp);
     rc = tensor_map_2d(&ta, w.G, 1, b.Vc / 64 * b.Tp, 64, 64, KB * p.kps, 128);
     if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, w.Hc, 1, b.Tp, D, b.Dp, KB * p.kps, 128);
-    if (rc == EFQAT_OK) rc = tensor_map_2d(&to, dW + v0 * D, 1, nv, D, D, 32, 64);
-    if (rc == EFQAT_OK) rc = launch<1, 1, LM_DW>(p, t, ta, tb, to, sm_count, st);
+    p.out = dW + v0 * D;
+    if (rc == EFQAT_OK) rc = launch<1, 1, LM_DW>(p, t, ta, tb, ta, sm_count, st);
     if (rc != EFQAT_OK) return rc;
   }
   const int groups = b.splits >= 8 ? 8 : 1;
