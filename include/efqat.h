@@ -327,8 +327,8 @@ int efqat_layer_norm_recompute(efqat_ctx* ctx, int dtype, const efqat_ckpt* save
  *   G[t,v] = dloss[t] * (exp(l[t,v] - lse[t]) - [v = label])
  *   dH = G W  bf16 [T,D],   dW = G^T H  bf16 [V,D]   (both written whole; fixed order of all sums).
  * G / max|dloss| is rounded to bf16 as the operand of the two products; sums are fp32, dH and dW
- * are rounded once.  V and T may be any size (T = 0: dW is zeroed), D % 8 == 0; T, V <= 2^24 and
- * D <= 2^20.  The workspace of the backward holds one piece of G, at most about 256 MiB, a copy of
+ * are rounded once.  V and T may be any size (T = 0: dW is zeroed), D % 8 == 0; T, V <= 2^24,
+ * D <= 2^20 and T * V < 2^44.  The workspace of the backward holds one piece of G, at most about 256 MiB, a copy of
  * the hidden states that have a target and fp32 sums of dH. */
 int efqat_lm_loss_workspace_bytes(int64_t T, int64_t V, int64_t D, size_t* fwd_bytes, size_t* bwd_bytes);
 int efqat_lm_loss_fwd(efqat_ctx* ctx, const void* H, const void* W, const int32_t* labels, int64_t T, int64_t V,

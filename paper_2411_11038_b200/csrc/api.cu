@@ -1198,6 +1198,8 @@ static int check_lm(int64_t T, int64_t V, int64_t D) {
   if (D & 7) return EFQAT_ERR_ALIGN;
   // row and column numbers of every matrix, and of the fp32 partial sums, stay within 2^30
   if (T > (1 << 24) || V > (1 << 24) || D > (1 << 20)) return EFQAT_ERR_TOO_LARGE;
+  // the work list of the logits (tiles of 128 x 64 at least) is numbered in 31 bits
+  if (ceil_div(T, 128) * ceil_div(V, 64) > INT32_MAX) return EFQAT_ERR_TOO_LARGE;
   return EFQAT_OK;
 }
 

@@ -180,7 +180,8 @@ def test_lm_loss_queries(lib):
     fwd, bwd = B.lm_loss_workspace_bytes(8192, 128000, 2048)
     assert fwd < 8192 * 128000 * 4 // 32 and bwd < 8192 * 128000 * 2 // 4
     assert B.lm_loss_workspace_bytes(0, 100, 64) == (0, 0)
-    for args, code in (((4, 0, 64), -2), ((-1, 10, 64), -2), ((4, 10, 60), -3), ((4, 1 << 25, 64), -11)):
+    for args, code in (((4, 0, 64), -2), ((-1, 10, 64), -2), ((4, 10, 60), -3), ((4, 1 << 25, 64), -11),
+                       ((1 << 24, 1 << 24, 64), -11)):
         with pytest.raises(B.EfqatError) as e:
             B.lm_loss_workspace_bytes(*args)
         assert e.value.code == code
