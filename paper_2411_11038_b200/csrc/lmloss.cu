@@ -495,6 +495,96 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   }
 }
 
+// One token: W is streamed once, rows by warps, with plain loads; a tile of the tensor cores would be
+// empty but for one row, and its ring takes longer to fill.  A warp takes 4 rows at a time, a lane 16
+// columns of them per step against the hidden state in shared memory, in packed fp32 (a product of two
+// bf16 is exact there); lane r keeps the running maximum and sum of the r-th rows.  One partial per block.
+// 32000 x 1024: 12.0 us with its combine against 16.1 through the tiles; 128000 x 2048: 80.4 against 88.9
+// (the copy rate).  2 or 8 rows a warp, or 3 or 6 blocks an SM, are slower at 65 MB.  With two tokens the
+// products bound it (26 us against 16), which is why it is for one only.
+static const int ONE_WARPS = 8, ONE_ROWS = 4;
+
+__global__ void __launch_bounds__(32 * ONE_WARPS, 4) lm_one_kernel(const bf16* __restrict__ h_row, const bf16* __restrict__ W,
+                                                                   const int32_t* __restrict__ labels, int64_t V, int D,
+                                                                   int wide, float2* __restrict__ part,
+                                                                   float* __restrict__ label_logit) {
+  extern __shared__ __align__(16) uint8_t one_smem[];
+  __shared__ float2 s_part[ONE_WARPS];
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint4* h = reinterpret_cast<uint4*>(one_smem);                    // [D / 8]
+  for (int i = threadIdx.x; i < D / 8; i += 32 * ONE_WARPS) h[i] = reinterpret_cast<const uint4*>(h_row)[i];
+  const int label = labels[0];
+  __syncthreads();
+  float m = -INFINITY, sum = 0.f;
+  for (int64_t v0 = (static_cast<int64_t>(blockIdx.x) * ONE_WARPS + warp) * ONE_ROWS; v0 < V;
+       v0 += static_cast<int64_t>(gridDim.x) * ONE_WARPS * ONE_ROWS) {
+    pair_t acc[ONE_ROWS] = {0, 0, 0, 0};
+#pragma unroll 1                                                    // (two steps at once do not fit the registers)
+    for (int c = lane * 16; c < D; c += 512) {
+      uint4 w[ONE_ROWS][2];
+#pragma unroll
+      for (int r = 0; r < ONE_ROWS; ++r) {
+        w[r][0] = w[r][1] = make_uint4(0, 0, 0, 0);
+        const bf16* p = W + (v0 + r) * D + c;
+        if (v0 + r < V) {
+          if (wide) {
+            load32(p, 1, w[r][0], w[r][1]);
+          } else {
+            w[r][0] = *reinterpret_cast<const uint4*>(p);
+            if (c + 8 < D) w[r][1] = *reinterpret_cast<const uint4*>(p + 8);
+          }
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        pair_t x[4];
+        unpack8(c + 8 * q < D ? h[c / 8 + q] : make_uint4(0, 0, 0, 0), x);
+#pragma unroll
+        for (int r = 0; r < ONE_ROWS; ++r) {
+          pair_t y[4];
+          unpack8(w[r][q], y);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[r] = fma2(x[i], y[i], acc[r]);
+        }
+      }
+    }
+    float mine = 0.f;
+#pragma unroll
+    for (int r = 0; r < ONE_ROWS; ++r) {
+      const float2 a = halves(acc[r]);
+      const float l = warp_sum(a.x + a.y);
+      if (lane == r) mine = l;
+    }
+    if (lane < ONE_ROWS && v0 + lane < V) {
+      if (v0 + lane == label) label_logit[0] = mine;
+      const float m1 = fmaxf(m, mine);
+      sum = (m == -INFINITY ? 0.f : sum * ex2((m - m1) * LOG2E)) + ex2((mine - m1) * LOG2E);
+      m = m1;
+    }
+  }
+  // the warp's lanes, then the block's warps; what saw no row has the sum 0 and the maximum -inf
+  float top = m;
+#pragma unroll
+  for (int o = ONE_ROWS / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float v = sum == 0.f ? 0.f : sum * ex2((m - top) * LOG2E);
+#pragma unroll
+  for (int o = ONE_ROWS / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane == 0) s_part[warp] = make_float2(top, v);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    top = -INFINITY;
+    v = 0.f;
+    for (int w = 0; w < ONE_WARPS; ++w) top = fmaxf(top, s_part[w].x);
+    for (int w = 0; w < ONE_WARPS; ++w) {
+      const float2 o = s_part[w];
+      if (o.y != 0.f) v += o.y * ex2((o.x - top) * LOG2E);      // (NaN is not 0)
+    }
+    part[blockIdx.x] = make_float2(top, v);
+  }
+}
+
 // lse and loss of each token from the partial maxima and sums: 16 tokens per block, 64 threads each.
 __global__ void __launch_bounds__(1024) lm_combine_kernel(const float2* __restrict__ part, int parts, int64_t pitch,
                                                           const float* __restrict__ label_logit,
@@ -771,7 +861,7 @@ struct FwdWs {
   float2* part; float* label_logit;
   size_t bytes;
 };
-FwdWs carve_fwd(void* ws, int64_t T, int64_t tiles_n) {
+FwdWs carve_fwd(void* ws, int64_t T, int64_t parts) {
   FwdWs w = {};
   char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(ws) + 255) & ~uintptr_t(255));
   size_t off = 0;
@@ -780,7 +870,7 @@ FwdWs carve_fwd(void* ws, int64_t T, int64_t tiles_n) {
     off += static_cast<size_t>(round_up(bytes, 256));
     return r;
   };
-  w.part = reinterpret_cast<float2*>(take(2 * tiles_n * T * 8));
+  w.part = reinterpret_cast<float2*>(take(parts * T * 8));
   w.label_logit = reinterpret_cast<float*>(take(T * 4));
   w.bytes = off + 256;
   return w;
@@ -866,15 +956,48 @@ int lm_loss_init() {
   return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
 
+// One token, its hidden state within the shared memory of a quarter of an SM (no more than a block has
+// without asking for it).
+static bool one_token(int64_t T, int64_t D) { return T == 1 && D <= 20 * 1024; }
+
+// Blocks of the one-token forward: four to an SM, every warp with the same number of row groups.
+static int64_t one_grid(int64_t V, int sm_count) {
+  const int64_t groups = ceil_div(V, ONE_ROWS), warps = static_cast<int64_t>(sm_count) * 4 * ONE_WARPS;
+  return ceil_div(groups, ONE_WARPS * ceil_div(groups, warps));
+}
+
+// Partials per token of the forward.
+static int64_t fwd_parts(int64_t T, int64_t V, int64_t D, int sm_count) {
+  return one_token(T, D) ? one_grid(V, sm_count) : 2 * choose_tiling(T, V, 32, sm_count).tiles_n;
+}
+
 void lm_loss_workspace_bytes(int64_t T, int64_t V, int64_t D, int sm_count, size_t* fwd, size_t* bwd) {
-  *fwd = carve_fwd(nullptr, T, choose_tiling(T, V, 32, sm_count).tiles_n).bytes;
+  *fwd = carve_fwd(nullptr, T, fwd_parts(T, V, D, sm_count)).bytes;
   *bwd = carve_bwd(nullptr, bwd_plan(T, V, D, sm_count), T, D).bytes;
+}
+
+static int combine(const FwdWs& w, int64_t parts, const int32_t* labels, int64_t T, int64_t V, float* loss, float* lse,
+                   int* status, cudaStream_t st) {
+  count_launches(1);
+  return launch_dependent(lm_combine_kernel, static_cast<unsigned>(ceil_div(T, 16)), 1024, 0, st, 1,
+                          static_cast<const float2*>(w.part), static_cast<int>(parts), T,
+                          static_cast<const float*>(w.label_logit), labels, T, V, loss, lse, status) == cudaSuccess
+             ? EFQAT_OK : EFQAT_ERR_CUDA;
 }
 
 int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t T, int64_t V, int64_t D, float* loss,
                     float* lse, void* ws, int* status, int sm_count, cudaStream_t st) {
+  const int64_t parts = fwd_parts(T, V, D, sm_count);
+  const FwdWs w = carve_fwd(ws, T, parts);
+  if (one_token(T, D)) {
+    const int wide = D % 16 == 0 && (reinterpret_cast<uintptr_t>(W) & 31) == 0;
+    count_launches(1);
+    if (launch_dependent(lm_one_kernel, static_cast<unsigned>(parts), 32u * ONE_WARPS, static_cast<size_t>(D * 2), st, 1, H, W, labels, V,
+                         static_cast<int>(D), wide, w.part, w.label_logit) != cudaSuccess)
+      return EFQAT_ERR_CUDA;
+    return combine(w, parts, labels, T, V, loss, lse, status, st);
+  }
   const Tiling t = choose_tiling(T, V, 32, sm_count);
-  const FwdWs w = carve_fwd(ws, T, t.tiles_n);
   CUtensorMap ta, tb;
   int rc = tensor_map_2d(&ta, H, 1, T, D, D, token_box(T), 128);
   if (rc == EFQAT_OK) rc = tensor_map_2d(&tb, W, 1, V, D, D, t.pair ? t.BN / 2 : t.BN, 128);
@@ -889,12 +1012,7 @@ int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t
   p.status = status;
   set_ring(&p, t, false, token_box(T));
   rc = launch<0, 0, LM_STAT>(p, t, ta, tb, ta, sm_count, st);
-  if (rc != EFQAT_OK) return rc;
-  count_launches(1);
-  return launch_dependent(lm_combine_kernel, static_cast<unsigned>(ceil_div(T, 16)), 1024, 0, st, 1,
-                          static_cast<const float2*>(w.part), static_cast<int>(2 * t.tiles_n), T,
-                          static_cast<const float*>(w.label_logit), labels, T, V, loss, lse, status) == cudaSuccess
-             ? EFQAT_OK : EFQAT_ERR_CUDA;
+  return rc != EFQAT_OK ? rc : combine(w, parts, labels, T, V, loss, lse, status, st);
 }
 
 int run_lm_loss_bwd(const bf16* H, const bf16* W, const int32_t* labels, const float* lse, const float* dloss,

@@ -92,6 +92,30 @@ def test_loss_and_gradients(ctx, T, V, D):
     check(ctx, T, V, D, T + V + D)
 
 
+@pytest.mark.parametrize("V,D", [(1, 8), (3, 24), (4, 512), (31, 520), (32000, 1024), (50259, 1000), (9001, 16),
+                                 (700, 20480), (700, 20488)])
+def test_one_token(ctx, V, D):
+    """A single token: rows of W shorter and longer than a warp's step, not a multiple of 32 bytes, and hidden states
+    on both sides of the length that a block keeps in shared memory."""
+    check(ctx, 1, V, D, V + D, ignore=0.0)
+
+
+def test_one_token_offset_and_nan(ctx):
+    """The same weights at an address that is a multiple of 16 but not of 32 bytes; a NaN in a row of W."""
+    V, D = 5003, 256
+    H, W, labels, _ = make(1, V, D, 4, ignore=0.0)
+    flat = torch.zeros(V * D + 16, dtype=torch.bfloat16, device="cuda")
+    odd = flat[8:8 + V * D].view(V, D)
+    odd.copy_(W)
+    assert odd.data_ptr() % 32 == 16
+    plan = B.LmLossPlan(ctx, 1, V, D, "cuda", backward=False)
+    want = plan.fwd(H, W, labels).clone()
+    assert torch.equal(plan.fwd(H, odd, labels), want)
+    W[4999, 17] = float("nan")
+    assert torch.isnan(plan.fwd(H, W, labels)).all() and torch.isnan(plan.lse).all()
+    assert ctx.device_status() == 0
+
+
 def test_several_pieces_of_the_vocabulary(ctx):
     """A vocabulary that takes three pieces of G (256 MiB each at most), the last one narrower."""
     T, V, D = 12288, 30001, 72
