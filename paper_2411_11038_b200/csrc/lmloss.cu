@@ -14,9 +14,16 @@
 // The logits of the backward are formed a second time from the stored lse: 2 of its 6 TVD
 // multiply-adds, instead of T V values kept from the forward.
 //
-// G lies in panels of 64 columns, each a dense [tokens x 64] matrix: a k-block of either product that reads
-// it is one contiguous piece of 16 KB.  (With plain rows, 128 of them contribute 128 bytes each to a
-// k-block of DH, and the product ran at 880 TFLOP/s.)
+// What bounds the four: the operands' way from L2 into shared memory, 11.8 TB/s with 256 x 256 tiles, and
+// the clock, which the power limit holds at 1.45 to 1.5 GHz of 1.965.  8192 tokens x 128000 x 2048: forward
+// 2.83 ms = 1.52 PFLOP/s, backward (90 % of the tokens with a target) 8.9 ms.  The tensor pipe is busy 81 %
+// of the cycles in STAT, 77 % in GRAD, 82 to 85 % in DH and 87 % in DW.  Boxes prefetched into L2 one ring
+// ahead (5 to 20 % slower), one or three k-blocks per stage and a STAT without its epilogue (3 to 6 %
+// faster) say that neither latency nor the epilogue is the bound.
+//
+// G lies in panels of 64 columns, each a dense [tokens x 64] matrix: GRAD's stores of neighbouring rows are
+// then neighbours in memory (8 % of GRAD), and a k-block of DH or DW is one contiguous piece of 16 KB (which
+// makes no difference to them).
 //
 // G holds p - [v = label] times d_t / max|d|: the common factor max|d| is applied in fp32 behind the
 // products, so that the mean's 1 / n, the same for every token, costs no rounding.  Tokens without a

@@ -8,14 +8,19 @@
 // HBM-bound: every tensor is touched once.  A row belongs to a team of 1, 2, 4, 8 or 16 warps, a lane to up
 // to 32 of its columns (8 or 16 lanes and one warp where rows are short).
 //
-// Forward: the simplest form at the highest occupancy, one row per team and no loop.  (A persistent
-// form with rows prefetched into shared memory was measured too: 16 warps with their row's chain of
-// reductions do not cover an SM's share of the bandwidth; 16384 x 4096 bf16 47.6 us.)
+// Forward: the simplest form at the highest occupancy, one row per team and no loop; the other blocks of the
+// SM cover a row's chain of load, two reductions and store.  16384 x 4096 (B200): bf16 48.0 us (86 % of the
+// copy rate), with the checkpoint 63 us (82 %), fp32 83 us (100 %); 9216 x 1024 bf16 10.0 us (59 %: launch,
+// ramp and tail are half of it).  Persistent blocks with rows prefetched into shared memory, 16 warps per SM,
+// measured 47.6, 66 and 98 us, 65536 x 256 bf16 19 us against 14.7 and 4093 x 1040 fp32 12 us against 9.4.
 //
 // Backward: persistent blocks, one per SM, since dgamma and dbeta want each lane to keep its columns: their
 // running sums stay in registers over all rows of the team.  Each team keeps a ring of its next rows
 // in shared memory, filled by bulk copies that it requests itself as soon as it has read a row;
-// teams of one warp (up to 1024 columns) never wait for each other.
+// teams of one warp (up to 1024 columns) never wait for each other.  16384 x 4096: bf16 74 us (83 % of the copy
+// rate), fp32 136 us (90 %), from the checkpoint 80 us (64 %: widening the codes joins the issue slots that
+// bound it).  9216 x 1024: 17.5 us, of which the launch that adds the blocks' partial sums is 2 to 4.
+// 12 or 16 warps leave a lane too few registers for its sums and spill; rows kept as raw bits measured the same.
 //
 // A warp forms the variance around the mean of its own columns, and the warps' parts are joined
 // exactly (M2 = sum M2_w + sum n_w (mean_w - mean)^2): no cancellation for rows far from zero, one
@@ -194,16 +199,6 @@ struct Raw {
       const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(x) + at);
       r[0] = p[0];
       if (sizeof(T) == 4) r[sizeof(r) / 16 - 1] = p[1];
-    }
-  }
-  __device__ __forceinline__ void load_shared(uint32_t addr) {
-    if (SRC) {
-      const uint2 w = lds64(addr);
-      r[0].x = w.x;
-      r[0].y = w.y;
-    } else {
-      r[0] = lds128(addr);
-      if (sizeof(T) == 4) r[sizeof(r) / 16 - 1] = lds128(addr + 16);
     }
   }
   __device__ __forceinline__ void get(float scale, pair_t (&v)[4]) const {

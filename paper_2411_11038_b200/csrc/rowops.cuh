@@ -84,7 +84,6 @@ template <>
 struct Vec8<bf16> {
   uint4 r;
   __device__ __forceinline__ void load(const bf16* p) { r = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { r = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void get(pair_t (&v)[4]) const { unpack8(r, v); }
 };
 template <>
@@ -94,7 +93,6 @@ struct Vec8<float> {
     r = reinterpret_cast<const uint4*>(p)[0];
     q = reinterpret_cast<const uint4*>(p)[1];
   }
-  __device__ __forceinline__ void zero() { r = q = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void get(pair_t (&v)[4]) const { unpack8(r, q, v); }
 };
 
