@@ -6,7 +6,8 @@
 //
 // Everything heavy is one of four matrix products on the tensor cores; what follows a product
 // happens on its accumulator in the epilogue, so a logit never leaves the SM:
-//   STAT  l = H W^T     -> per row and half tile the running maximum and sum of exponentials
+//   STAT  l = H W^T     -> per row and half tile the running maximum and sum of exponentials (STAT_LONG:
+//                          contractions above 1024, summed in segments)
 //   GRAD  l = H Wc^T    -> G of one piece of the vocabulary, rounded to bf16 (an operand)
 //   DH    G Wc          -> added to fp32 sums of dH (bulk reductions in L2; one add per piece, in
 //                          stream order, so the sums have a fixed order)
@@ -16,7 +17,7 @@
 //
 // What bounds the four: the operands' way from L2 into shared memory, 11.8 TB/s with 256 x 256 tiles, and
 // the clock, which the power limit holds at 1.45 to 1.5 GHz of 1.965.  8192 tokens x 128000 x 2048: forward
-// 2.83 ms = 1.52 PFLOP/s, backward (90 % of the tokens with a target) 8.9 ms.  The tensor pipe is busy 81 %
+// 3.37 ms = 1.27 PFLOP/s in a long run, backward (90 % of the tokens with a target) 8.9 ms.  The tensor pipe is busy 81 %
 // of the cycles in STAT, 77 % in GRAD, 82 to 85 % in DH and 87 % in DW.  Boxes prefetched into L2 one ring
 // ahead (5 to 20 % slower), one or three k-blocks per stage and a STAT without its epilogue (3 to 6 %
 // faster) say that neither latency nor the epilogue is the bound.
@@ -42,7 +43,7 @@ using namespace ptx;
 
 namespace {
 
-enum { LM_STAT = 0, LM_GRAD = 1, LM_DH = 2, LM_DW = 3 };
+enum { LM_STAT = 0, LM_GRAD = 1, LM_DH = 2, LM_DW = 3, LM_STAT_LONG = 4 };
 
 static const int ROWS = 128;                    // rows of a CTA's tile = TMEM lanes
 static const int KB = 64;                       // contraction elements per k-block (one 128-byte swizzle row)
@@ -53,6 +54,11 @@ static const int WORKERS = 8;                   // epilogue warps
 static const int THREADS = 64 + 32 * WORKERS;
 static const int ACC_COLS = 256, TMEM_ALL = 512;
 static const int STG_BYTES = 32 * 64;           // staging block of one epilogue warp: 32 rows x 64 bytes
+// The tensor core's running sums lose their low bits by truncation, always towards zero: the mean loss over 128000
+// x 2048 came out 1.8e-5 too small (1.2e-6 of it), over 4096 columns 3.6e-5.  So the forward's accumulators end
+// after 1024 columns and the epilogue adds them in fp32: 5.3e-7 for either, at 4 % of the forward (3.24 -> 3.37 ms).
+// G is rounded to bf16 right away; the logits behind it stay in one piece.
+static const int SEG_KB = 16;
 static const float LOG2E = 1.4426950408889634f;
 
 // What the epilogues need to know of a token with a target.
@@ -70,7 +76,8 @@ struct LmParams {
   int BN, kps, stages, splits;
   int panel;                  // tile columns walked row block by row block (order of the work list)
   int a_kb_tx, b_kb_bytes;    // bytes that a k-block's copies of A and of B bring
-  // STAT
+  // STAT, STAT_LONG
+  int seg_kb;                 // k-blocks of a segment of the contraction (a multiple of kps)
   const int32_t* labels;
   float2* part; float* label_logit; int64_t part_pitch;
   // GRAD
@@ -136,6 +143,7 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
   const int unit = PAIR ? (blockIdx.x >> 1) : blockIdx.x;
   const int units = PAIR ? (gridDim.x >> 1) : gridDim.x;
   constexpr int TILE_M = PAIR ? 2 * ROWS : ROWS;
+  constexpr bool STAT = EPI == LM_STAT || EPI == LM_STAT_LONG;
   const int bn_cta = PAIR ? (p.BN >> 1) : p.BN;
 
   if (threadIdx.x == 0) {
@@ -264,10 +272,16 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
       const uint32_t a_lbo = A_MN ? p.kps * CHUNK : 16, b_lbo = B_MN ? p.kps * CHUNK : 16;
       const uint32_t a_step = A_MN ? CHUNK : A_KB_BYTES, b_step = B_MN ? CHUNK : p.b_kb_bytes;
       const uint32_t ring = smem_u32(smem);
-      for (int w = unit; w < items && ok; w += units, ++acc_it) {
-        const int split = p.splits > 1 ? w / tiles : 0;
-        const int kb0 = static_cast<int>(static_cast<int64_t>(split) * nkb / p.splits);
-        const int kb1 = static_cast<int>(static_cast<int64_t>(split + 1) * nkb / p.splits);
+      // An accumulator per item; STAT_LONG: one per segment of an item's contraction.
+      int kb0 = 0, kb1 = 0, end = 0;
+      for (int w = unit; w < items && ok; w += kb1 == end ? units : 0, ++acc_it) {
+        if (kb1 == end) {
+          const int split = p.splits > 1 ? w / tiles : 0;
+          kb1 = static_cast<int>(static_cast<int64_t>(split) * nkb / p.splits);
+          end = static_cast<int>(static_cast<int64_t>(split + 1) * nkb / p.splits);
+        }
+        kb0 = kb1;
+        kb1 = EPI == LM_STAT_LONG && end - kb0 > p.seg_kb ? kb0 + p.seg_kb : end;
         const int buf = acc_it & 1;
         if (*abort_flag || !mbar_wait(&ctl->acc_empty[buf], ((acc_it >> 1) & 1) ^ 1)) {
           record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
@@ -327,12 +341,11 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
       int tm, tn;
       tile_at(w - split * tiles, tiles_m, tiles_n, p.panel, tm, tn);
       const int row0 = tm * TILE_M + rank * ROWS + q * 32, row = row0 + lane, n0 = tn * p.BN;
-      const int buf = acc_it & 1;
       // this thread's token, fetched behind the products
       int label = -1;
       float nlse2 = 0.f, ratio = 0.f;
       bool live = false;
-      if (EPI == LM_STAT) {
+      if (STAT) {
         live = row < p.Mr;
         if (live) label = p.labels[row];
       } else if (EPI == LM_GRAD) {
@@ -344,15 +357,20 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
           label = r.label - p.v0;
         }
       }
-      bool got = *abort_flag ? false : mbar_wait(&ctl->acc_full[buf], (acc_it >> 1) & 1);
-      got = __all_sync(0xffffffffu, got);
-      if (!got) {
-        record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
-        *abort_flag = 1;
-        break;
-      }
-      tc_fence_after();
-      const uint32_t t_row = tmem_base + buf * ACC_COLS + (static_cast<uint32_t>(q * 32) << 16);
+      int buf = acc_it & 1;
+      uint32_t t_row = 0;
+      auto take = [&]() {                            // waits for the next accumulator
+        buf = acc_it & 1;
+        t_row = tmem_base + buf * ACC_COLS + (static_cast<uint32_t>(q * 32) << 16);
+        bool got = *abort_flag ? false : mbar_wait(&ctl->acc_full[buf], (acc_it >> 1) & 1);
+        got = __all_sync(0xffffffffu, got);
+        if (!got) {
+          record_status(p.status, EFQAT_DEV_WAIT_TIMEOUT);
+          *abort_flag = 1;
+        }
+        tc_fence_after();
+        return got;
+      };
       // Hands the accumulator back, once this warp's last columns are in registers.
       bool released = false;
       auto release = [&]() {
@@ -364,39 +382,77 @@ lm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
           else mbar_arrive(&ctl->acc_empty[buf]);
         }
       };
+      // STAT_LONG: the sums of the segments, added up here with fp32's own rounding.  16 columns at a time, since
+      // the thread's 128 sums leave no more registers.
+      float z[EPI == LM_STAT_LONG ? 4 : 1][32];
+      auto add_segment = [&](int i, int h, bool first) {
+        uint32_t r[32];
+        tmem_ld_32x16(t_row + (jb0 + i) * 32 + h * 16, r);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          z[i][h * 16 + j] = first ? __uint_as_float(r[j]) : z[i][h * 16 + j] + __uint_as_float(r[j]);
+      };
+      bool stop = false;
+      if constexpr (EPI == LM_STAT_LONG) {
+        for (int kb = p.seg_kb; kb < nkb; kb += p.seg_kb, ++acc_it) {
+          stop = !take();
+          if (stop) break;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (jb0 + i / 2 < jb1) add_segment(i / 2, i & 1, kb == p.seg_kb);
+          release();
+        }
+        released = false;
+      }
+      if (stop || !take()) break;
       const int64_t cols = EPI == LM_GRAD ? (p.Nc + 63) & ~int64_t(63) : p.Nc;      // G: whole panels
       auto last_block = [&](int jb) { return jb + 1 == jb1 || n0 + (jb + 1) * BC >= cols; };
-      if (EPI == LM_STAT) {
+      if constexpr (STAT) {
         float m = -INFINITY, sum = 0.f;
-        for (int jb = jb0; jb < jb1; ++jb) {
-          const int c0 = n0 + jb * 32;
-          if (c0 >= p.Nc) break;
-          uint32_t r[32];
-          tmem_ld_32x32(t_row + jb * 32, r);
-          tmem_wait_ld();
-          if (last_block(jb)) release();
+        auto consume = [&](float (&v)[32], int c0) {
           if (c0 + 32 > p.Nc) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (c0 + j >= p.Nc) r[j] = 0xff800000u;      // columns past the vocabulary: exp gives 0
+              if (c0 + j >= p.Nc) v[j] = -INFINITY;        // columns past the vocabulary: exp gives 0
           }
           const int at = label - c0;
           if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (at == j) p.label_logit[row] = __uint_as_float(r[j]);
+              if (at == j) p.label_logit[row] = v[j];
           }
           // four chains each: a chain of 32 would be the epilogue's time on the last tile
-          float top[4], part[4] = {0.f, 0.f, 0.f, 0.f};
+          float top[4] = {v[0], v[1], v[2], v[3]}, part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) top[j] = __uint_as_float(r[j]);
-#pragma unroll
-          for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], __uint_as_float(r[j]));
+          for (int j = 4; j < 32; ++j) top[j & 3] = fmaxf(top[j & 3], v[j]);
           const float m1 = fmaxf(fmaxf(m, fmaxf(top[0], top[1])), fmaxf(top[2], top[3])), off = -m1 * LOG2E;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) part[j & 3] += ex2(fmaf(__uint_as_float(r[j]), LOG2E, off));
+          for (int j = 0; j < 32; ++j) part[j & 3] += ex2(fmaf(v[j], LOG2E, off));
           sum = (m == -INFINITY ? 0.f : sum * ex2(fmaf(m, LOG2E, off))) + ((part[0] + part[1]) + (part[2] + part[3]));
           m = m1;
+        };
+        if constexpr (EPI == LM_STAT_LONG) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int jb = jb0 + i, c0 = n0 + jb * 32;
+            if (jb < jb1 && c0 < p.Nc) {
+              add_segment(i, 0, false);
+              add_segment(i, 1, false);
+              if (last_block(jb)) release();
+              consume(z[i], c0);
+            }
+          }
+        } else {
+          for (int jb = jb0; jb < jb1 && n0 + jb * 32 < p.Nc; ++jb) {
+            uint32_t r[32];
+            tmem_ld_32x32(t_row + jb * 32, r);
+            tmem_wait_ld();
+            if (last_block(jb)) release();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z[0][j] = __uint_as_float(r[j]);
+            consume(z[0], n0 + jb * 32);
+          }
         }
         if (live) p.part[static_cast<int64_t>(tn * 2 + half) * p.part_pitch + row] = make_float2(m, sum);
       } else if (EPI == LM_GRAD) {
@@ -957,7 +1013,8 @@ int panel_of(const Tiling& t, int64_t contraction) {
 }  // namespace
 
 int lm_loss_init() {
-  const bool ok = allow<0, 0, LM_STAT, 0>() && allow<0, 0, LM_STAT, 1>() && allow<0, 0, LM_GRAD, 0>() &&
+  const bool ok = allow<0, 0, LM_STAT, 0>() && allow<0, 0, LM_STAT, 1>() && allow<0, 0, LM_STAT_LONG, 0>() &&
+                  allow<0, 0, LM_STAT_LONG, 1>() && allow<0, 0, LM_GRAD, 0>() &&
                   allow<0, 0, LM_GRAD, 1>() && allow<0, 1, LM_DH, 0>() && allow<0, 1, LM_DH, 1>() &&
                   allow<1, 1, LM_DW, 0>() && allow<1, 1, LM_DW, 1>();
   return ok ? EFQAT_OK : EFQAT_ERR_CUDA;
@@ -1018,7 +1075,9 @@ int run_lm_loss_fwd(const bf16* H, const bf16* W, const int32_t* labels, int64_t
   p.part = w.part; p.label_logit = w.label_logit; p.part_pitch = T;
   p.status = status;
   set_ring(&p, t, false, token_box(T));
-  rc = launch<0, 0, LM_STAT>(p, t, ta, tb, ta, sm_count, st);
+  const int64_t segs = ceil_div(p.nkb, SEG_KB);
+  p.seg_kb = static_cast<int>(round_up(ceil_div(p.nkb, segs), p.kps));
+  rc = segs > 1 ? launch<0, 0, LM_STAT_LONG>(p, t, ta, tb, ta, sm_count, st) : launch<0, 0, LM_STAT>(p, t, ta, tb, ta, sm_count, st);
   return rc != EFQAT_OK ? rc : combine(w, parts, labels, T, V, loss, lse, status, st);
 }
 

@@ -92,6 +92,12 @@ def test_loss_and_gradients(ctx, T, V, D):
     check(ctx, T, V, D, T + V + D)
 
 
+@pytest.mark.parametrize("T,V,D", [(130, 700, 1032), (300, 999, 2056), (9, 33, 1096), (520, 3001, 4096), (64, 300, 9000)])
+def test_long_contractions(ctx, T, V, D):
+    """Logits that are summed in segments of at most 1024 columns: two to nine of them, the last one shorter."""
+    check(ctx, T, V, D, T + D)
+
+
 @pytest.mark.parametrize("V,D", [(1, 8), (3, 24), (4, 512), (31, 520), (32000, 1024), (50259, 1000), (9001, 16),
                                  (700, 20480), (700, 20488)])
 def test_one_token(ctx, V, D):
