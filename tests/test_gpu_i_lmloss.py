@@ -122,6 +122,12 @@ def test_one_token_offset_and_nan(ctx):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("T,V,D", [(16, 9001, 1032), (260, 9001, 768), (580, 3001, 520), (1100, 5001, 200)])
+def test_slabs_joined(ctx, T, V, D):
+    """dH from many slabs of its contraction over the vocabulary, joined by 8, 4, 2 and 1 threads per column."""
+    check(ctx, T, V, D, T + 1)
+
+
 def test_several_pieces_of_the_vocabulary(ctx):
     """A vocabulary that takes three pieces of G (256 MiB each at most), the last one narrower."""
     T, V, D = 12288, 30001, 72
